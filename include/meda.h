@@ -41,7 +41,11 @@ typedef enum {
                                library's built-in array holds (MEDA_DECODE_NOALLOC_MAX_BYTES)        */
 } meda_status;
 
-typedef enum { MEDA_F32 = 0, MEDA_BF16 = 1 } meda_dtype;
+typedef enum {
+  MEDA_F32 = 0,
+  MEDA_BF16 = 1,
+  MEDA_E4M3 = 2 /* 8-bit rows with one scale each (see meda_quantize_fp8): a type of pages only */
+} meda_dtype;
 
 /* flags */
 #define MEDA_FLAG_UNIFORM_BUDGET 1 /* skip the entropy softmax: S_l = B/L (+1 on the lowest layers)  */
@@ -232,6 +236,169 @@ meda_status meda_decode_attention_fp8(const meda_decode_params* params, const vo
                                       const int32_t* layer_len, const int64_t* layer_off, const void* k_new,
                                       const void* v_new, void* out, void* workspace, size_t workspace_bytes,
                                       void* hip_stream);
+
+/*
+ * ---- Paged cache: many requests that grow by a token per step ------------------------------------------------------
+ *
+ * The ragged cache of meda_compress cannot grow in place and belongs to one call.  To serve many requests the rows live
+ * in PAGES of page_size positions, drawn from one pool, and a block table names the pages of every request:
+ *   k_pages, v_pages  [n_pages][Hkv][page_size][d]; the pages of a pool are page_stride elements apart, so that K and V
+ *                     pages may lie next to each other in one buffer ([n_pages][2][Hkv][page_size][d])
+ *   k_scales, v_scales  [n_pages][Hkv][page_size] float, MEDA_E4M3 only (value = code * scale)
+ *   table             [R][max_blocks] int32: position p of row r is place p % page_size of page table[r][p / page_size]
+ *   slot              of a position, int64: page * page_size + place; -1: none
+ * A ROW of the table is one (sequence, layer) pair: the pass keeps another number of positions in every layer, so every
+ * layer has a length of its own.  The functions below take any set of rows; those of one layer are every L-th row of
+ * the table, lengths and slots (table_stride, len_stride, slot_stride).
+ *
+ * Every access is bounded on the device: a page number outside [0, n_pages) counts as a page without rows (attention
+ * skips its positions, writers write nothing there), a slot outside [0, n_pages * page_size) is skipped, a length is
+ * clamped to [0, max_blocks * page_size].  What lies behind a row's last position is never used and never written.
+ * Pages that two rows of one call write to, or slots that occur twice in one call, hold either value afterwards.
+ */
+typedef struct {
+  int64_t n_pages;     /* pages in the pool, 1 .. 2^31 - 1                                              */
+  int64_t page_stride; /* elements from one page to the next in k_pages and in v_pages; 0 = Hkv*page_size*d; otherwise
+                          at least that, and a multiple of 16 bytes                                     */
+  int32_t n_kv_heads;  /* Hkv, 1 .. 65535                                                               */
+  int32_t head_dim;    /* d: 64 or 128                                                                  */
+  int32_t page_size;   /* positions per page: 16, 32, 64, 128 or 256                                    */
+  int32_t dtype;       /* MEDA_F32, MEDA_BF16 or MEDA_E4M3                                              */
+  void* k_pages;       /* device pointers, 16-byte aligned                                              */
+  void* v_pages;
+  float* k_scales;     /* MEDA_E4M3: 4-byte aligned; otherwise ignored                                  */
+  float* v_scales;
+} meda_page_pool;
+
+/*
+ * Block tables and slot maps from request lengths.  For every row r with `len` = lens[r] positions, m = n_new[r]:
+ *   m < 0   the request has ended: its ceil(len / page_size) pages go back to the free pages, its length becomes 0
+ *   m >= 0  room for m more positions: the pages that ceil((len + m) / page_size) - ceil(len / page_size) blocks need are
+ *           taken from the free pages and entered into the table, the length becomes len + m
+ * A row is refused, its length and table unchanged, where len + m exceeds max_blocks * page_size (it then needs no pages),
+ * or where it needs pages and those needed by the rows up to and including it exceed the pages that were free when the call
+ * began (pages given back by the call serve the next one).
+ *   lens        [R] int32; lens_out [R] int32: the new lengths (may be lens itself)
+ *   table       [R][max_blocks] int32, updated in place
+ *   free_ring   [n_pages] int32, updated in place: the free pages lie at head, head + 1, .. (mod n_pages); pages are taken
+ *               at the head in row order and given back at the tail, in row and block order
+ *   free_state  [2] int64 {head, number of free pages}; free_state_out [2] may be free_state itself
+ *   slots       [R][max_new] int64: the slots of the first max_new new positions, -1 behind them; ignored with max_new = 0
+ *   granted     [R] int32: m, 0 for a refused row, -1 for an ended one; may be NULL
+ *   workspace   256-byte aligned, meda_page_update_workspace_bytes(n_rows) bytes
+ * A fresh pool is free_ring = 0 .. n_pages - 1, free_state = {0, n_pages}, lens = 0.  No page may be held twice.
+ * lens and lens_out, free_state and free_state_out are the same array or do not overlap.
+ */
+typedef struct {
+  int64_t n_pages;     /* 1 .. 2^31 - 1                                                                 */
+  int32_t n_rows;      /* R, 1 .. 65536; R * max_blocks < 2^31                                          */
+  int32_t max_blocks;  /* columns of the table, >= 1; max_blocks * page_size < 2^31                     */
+  int32_t page_size;   /* 16, 32, 64, 128 or 256                                                        */
+  int32_t max_new;     /* columns of slots, >= 0                                                        */
+} meda_page_params;
+size_t meda_page_update_workspace_bytes(int32_t n_rows);
+meda_status meda_page_update(const meda_page_params* params, const int32_t* lens, const int32_t* n_new, int32_t* table,
+                             int32_t* free_ring, const int64_t* free_state, int32_t* lens_out, int64_t* free_state_out,
+                             int64_t* slots, int32_t* granted, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Rotary positions with several axes (time, height, width of images and video; one axis for text).  Pair p < rot_dim / 2
+ * of a head's first rot_dim elements is turned by the angle positions[axis[p]][t] * inv_freq[p]:
+ *   (a, b) -> (a cos - b sin, b cos + a sin)
+ * The pairs are the elements (p, p + rot_dim / 2), or (2p, 2p + 1) with MEDA_ROTARY_INTERLEAVED; elements from rot_dim on
+ * pass unchanged.  MEDA_ROTARY_INVERSE turns back: the inverse of the rotation and its gradient (q = dL/dq_out gives
+ * q_out = dL/dq).  Angles are reduced in 64 bits, the turn is computed in fp32 and rounded once.
+ *   q, q_out, k, k_out   token t, head h at t * stride[0] + h * stride[1] (elements; the head_dim elements of a row are
+ *                        contiguous).  Any order: token-major projections in, [H][T][d] as meda_compress reads it out.
+ *                        An output may be its input (same pointer and strides), otherwise they do not overlap.
+ *                        k, k_out may be NULL with n_k_heads = 0, q and q_out with n_q_heads = 0.
+ *   positions            [n_axes][n_tokens] int32, an axis every pos_stride elements (0 = n_tokens)
+ *   inv_freq             [rot_dim / 2] double;  axis [rot_dim / 2] uint8, may be NULL with one axis (an axis number past
+ *                        the last axis counts as the last)
+ * Rows are moved in 16-byte pieces: pointers 16-byte aligned, strides multiples of 16 bytes.
+ */
+#define MEDA_ROTARY_INTERLEAVED 1
+#define MEDA_ROTARY_INVERSE 2
+typedef struct {
+  int64_t n_tokens;        /* 0 .. 2^26                                                                 */
+  int64_t q_stride[2], q_out_stride[2], k_stride[2], k_out_stride[2]; /* {token, head}, >= 0             */
+  int64_t pos_stride;
+  int32_t n_q_heads, n_k_heads; /* >= 0, at most 65535 together                                          */
+  int32_t head_dim;        /* d: 64 or 128                                                              */
+  int32_t rot_dim;         /* even, 2 .. d                                                              */
+  int32_t n_axes;          /* 1 .. 4                                                                    */
+  int32_t dtype;           /* MEDA_F32 or MEDA_BF16                                                     */
+  int32_t flags;           /* MEDA_ROTARY_*                                                             */
+} meda_rotary_params;
+meda_status meda_rotary(const meda_rotary_params* params, const void* q, const void* k, const int32_t* positions,
+                        const double* inv_freq, const uint8_t* axis, void* q_out, void* k_out, void* hip_stream);
+
+/*
+ * New tokens enter the pages: q and k are rotated as by meda_rotary (rot_dim = 0: they are not, and positions, inv_freq
+ * and axis are ignored), k and v are written to their slots.  dtype is the type of q, k, v and q_out: MEDA_F32 for pages of
+ * MEDA_F32, MEDA_BF16 for pages of MEDA_BF16 and MEDA_E4M3; a row of 8-bit pages is quantised from the fp32 values of the
+ * turn by the scheme of meda_quantize_fp8.  Strides, positions, inv_freq, axis and q_out = q as for meda_rotary.
+ *   q, q_out   [n_tokens][Hq][d] by their strides; NULL with n_q_heads = 0
+ *   k, v       [n_tokens][Hkv][d] by their strides
+ *   slots      int64, that of token t at t * slot_stride (0 = 1); a token without a slot (-1) is not written, its q is turned
+ */
+typedef struct {
+  int64_t n_tokens;        /* 0 .. 2^26                                                                 */
+  int64_t q_stride[2], q_out_stride[2], k_stride[2], v_stride[2];
+  int64_t pos_stride, slot_stride;
+  int32_t n_q_heads;       /* >= 0                                                                      */
+  int32_t rot_dim;         /* 0, or even, 2 .. d                                                        */
+  int32_t n_axes;          /* 1 .. 4 (ignored with rot_dim = 0)                                         */
+  int32_t dtype;
+  int32_t flags;           /* MEDA_ROTARY_INTERLEAVED                                                   */
+} meda_append_params;
+meda_status meda_paged_append(const meda_page_pool* pool, const meda_append_params* params, const void* q, const void* k,
+                              const void* v, const int32_t* positions, const double* inv_freq, const uint8_t* axis,
+                              const int64_t* slots, void* q_out, void* hip_stream);
+
+/*
+ * The compressed caches of a call of meda_compress move to pages: position i < min(layer_len[r], lens[r]) of row r = n * L + l
+ * (sequence n, layer l) goes to place i % page_size of page table[r][i / page_size], for every kv head.  `lens` are the
+ * lengths granted by meda_page_update: a refused row (0) is not stored.  Types as for meda_paged_append.
+ *   k_rows, v_rows  k_out, v_out of meda_compress; layer_len [N][L], layer_off [N][L+1] as it wrote them
+ *   lens            [N*L] int32, that of row r at r * len_stride; table: row r at r * table_stride
+ */
+typedef struct {
+  int64_t n_src_rows;      /* rows of k_rows and of v_rows (N * B * Hkv): none behind them is read      */
+  int64_t table_stride;    /* int32 entries from one row of the table to the next; 0 = max_blocks       */
+  int64_t len_stride;      /* 0 = 1                                                                     */
+  int32_t n_seqs;          /* N >= 1                                                                    */
+  int32_t n_layers;        /* L >= 1; N * L <= 65536                                                    */
+  int32_t max_blocks;      /* >= 1; max_blocks * page_size < 2^31, times Hkv <= 2^34                    */
+  int32_t dtype;           /* type of k_rows and v_rows                                                 */
+} meda_store_params;
+meda_status meda_paged_store(const meda_page_pool* pool, const meda_store_params* params, const void* k_rows,
+                             const void* v_rows, const int32_t* layer_len, const int64_t* layer_off, const int32_t* lens,
+                             const int32_t* table, void* hip_stream);
+
+/*
+ * Attention of one new token per row over its pages: out = Softmax(q K^T * scale) V over the first lens[r] positions, query
+ * head h reading kv head h / (Hq/Hkv); zeros where no position is left or every logit is -inf.  A value of +-inf in a position whose weight does
+ * not underflow gives +-inf in its column of out.
+ *   q, out   [R][Hq][d]; row r at r * q_stride and r * out_stride elements (0 = Hq * d), multiples of 16 bytes; `dtype`:
+ *            MEDA_F32 for pages of MEDA_F32, MEDA_BF16 for pages of MEDA_BF16 and MEDA_E4M3; out does not overlap q
+ *   table    row r at r * table_stride (0 = max_blocks); lens: that of row r at r * len_stride (0 = 1)
+ *   workspace  256-byte aligned, at least meda_paged_workspace_bytes(pool, params); what it holds before does not matter
+ * The work is cut evenly over the chip by the lengths, on the device: rows of very different lengths and a captured launch
+ * whose lengths grow are served alike.  A row's result depends on the other rows of the call by the rounding of fp32 sums.
+ */
+typedef struct {
+  int64_t q_stride, out_stride, table_stride, len_stride;
+  int32_t n_rows;          /* R, 1 .. 65536                                                             */
+  int32_t n_q_heads;       /* Hq, Hq % Hkv == 0, Hq / Hkv <= 16                                         */
+  int32_t max_blocks;      /* >= 1; max_blocks * page_size < 2^31, times Hkv <= 2^34                    */
+  int32_t dtype;
+  float softmax_scale;     /* 0 -> 1/sqrt(head_dim)                                                     */
+} meda_paged_params;
+size_t meda_paged_workspace_bytes(const meda_page_pool* pool, const meda_paged_params* params);
+meda_status meda_paged_attention(const meda_page_pool* pool, const meda_paged_params* params, const void* q,
+                                 const int32_t* table, const int32_t* lens, void* out, void* workspace,
+                                 size_t workspace_bytes, void* hip_stream);
 
 /*
  * Measurement aids for the benchmark: what this GPU delivers to the simplest kernel of each of the two kinds the

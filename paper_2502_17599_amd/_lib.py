@@ -15,7 +15,9 @@ EXPORTED_SYMBOLS = ("meda_workspace_bytes", "meda_compress", "meda_workspace_reg
                     "meda_profile_enable", "meda_profile_read", "meda_phase_name", "meda_status_string",
                     "meda_decode_workspace_bytes", "meda_decode_attention",
                     "meda_quantize_fp8", "meda_dequantize_fp8", "meda_decode_attention_fp8",
-                    "meda_decode_attention_noalloc", "meda_peak_stream_read", "meda_peak_mfma_bf16", "meda_peak_mfma_valu")
+                    "meda_decode_attention_noalloc", "meda_peak_stream_read", "meda_peak_mfma_bf16", "meda_peak_mfma_valu",
+                    "meda_page_update_workspace_bytes", "meda_page_update", "meda_rotary", "meda_paged_append",
+                    "meda_paged_store", "meda_paged_workspace_bytes", "meda_paged_attention")
 DECODE_NOALLOC_MAX_BYTES = 40 << 20
 REGIONS = {"col_scores": 0, "inv_norm": 1, "row_stats": 2, "alloc": 3, "less_idx": 4, "less_slot": 5}
 N_PHASES = 8
@@ -43,6 +45,45 @@ class MedaDecodeParams(ctypes.Structure):
     _fields_ = [("n_layers", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("n_new", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("total_budget", ctypes.c_int64), ("softmax_scale", ctypes.c_float)]
+
+
+class MedaPagePool(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int64), ("page_stride", ctypes.c_int64), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p)]
+
+
+class MedaPageParams(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int64), ("n_rows", ctypes.c_int32), ("max_blocks", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("max_new", ctypes.c_int32)]
+
+
+class MedaRotaryParams(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int64), ("q_stride", ctypes.c_int64 * 2), ("q_out_stride", ctypes.c_int64 * 2),
+                ("k_stride", ctypes.c_int64 * 2), ("k_out_stride", ctypes.c_int64 * 2), ("pos_stride", ctypes.c_int64),
+                ("n_q_heads", ctypes.c_int32), ("n_k_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("rot_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("flags", ctypes.c_int32)]
+
+
+class MedaAppendParams(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int64), ("q_stride", ctypes.c_int64 * 2), ("q_out_stride", ctypes.c_int64 * 2),
+                ("k_stride", ctypes.c_int64 * 2), ("v_stride", ctypes.c_int64 * 2), ("pos_stride", ctypes.c_int64),
+                ("slot_stride", ctypes.c_int64), ("n_q_heads", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("n_axes", ctypes.c_int32), ("dtype", ctypes.c_int32), ("flags", ctypes.c_int32)]
+
+
+class MedaStoreParams(ctypes.Structure):
+    _fields_ = [("n_src_rows", ctypes.c_int64), ("table_stride", ctypes.c_int64), ("len_stride", ctypes.c_int64),
+                ("n_seqs", ctypes.c_int32), ("n_layers", ctypes.c_int32), ("max_blocks", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class MedaPagedParams(ctypes.Structure):
+    _fields_ = [("q_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64), ("table_stride", ctypes.c_int64),
+                ("len_stride", ctypes.c_int64), ("n_rows", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("max_blocks", ctypes.c_int32), ("dtype", ctypes.c_int32), ("softmax_scale", ctypes.c_float)]
 
 
 def library_path() -> str:
@@ -98,6 +139,21 @@ def load_library() -> ctypes.CDLL:
     lib.meda_dequantize_fp8.argtypes = [vp, vp, ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, vp, vp]
     lib.meda_decode_attention_fp8.restype = ctypes.c_int
     lib.meda_decode_attention_fp8.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    pool = ctypes.POINTER(MedaPagePool)
+    lib.meda_page_update_workspace_bytes.restype = ctypes.c_size_t
+    lib.meda_page_update_workspace_bytes.argtypes = [ctypes.c_int32]
+    lib.meda_page_update.restype = ctypes.c_int
+    lib.meda_page_update.argtypes = [ctypes.POINTER(MedaPageParams)] + [vp] * 10 + [ctypes.c_size_t, vp]
+    lib.meda_rotary.restype = ctypes.c_int
+    lib.meda_rotary.argtypes = [ctypes.POINTER(MedaRotaryParams)] + [vp] * 8
+    lib.meda_paged_append.restype = ctypes.c_int
+    lib.meda_paged_append.argtypes = [pool, ctypes.POINTER(MedaAppendParams)] + [vp] * 9
+    lib.meda_paged_store.restype = ctypes.c_int
+    lib.meda_paged_store.argtypes = [pool, ctypes.POINTER(MedaStoreParams)] + [vp] * 7
+    lib.meda_paged_workspace_bytes.restype = ctypes.c_size_t
+    lib.meda_paged_workspace_bytes.argtypes = [pool, ctypes.POINTER(MedaPagedParams)]
+    lib.meda_paged_attention.restype = ctypes.c_int
+    lib.meda_paged_attention.argtypes = [pool, ctypes.POINTER(MedaPagedParams), vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     _lib = lib
     return lib
 

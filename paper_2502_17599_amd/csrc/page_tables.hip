@@ -1,0 +1,198 @@
+// Block tables and slot maps of a paged cache from the requests' lengths, and the pool's free pages.
+//
+// Every row asks for some pages (or gives its pages back).  Where a row's pages lie in the ring of free pages follows from
+// the sum of the needs of the rows before it: one scan over the rows, after which every entry of the table, the ring and
+// the slot map is computed on its own.  Pages are taken at the ring's head and given back at its tail: the entries read lie
+// in [head, head + free), those written in [head + free, head + free + given), and as no page is held twice the two never
+// meet in a ring of n_pages entries.  So nothing that one thread reads is written by another, except the lengths and the
+// ring's state themselves, which are written after everybody has read them.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/meda.h"
+#include "paged.hpp"
+
+namespace meda {
+
+struct PageUpdate {
+  const int32_t* lens;
+  const int32_t* n_new;
+  int32_t* table;
+  int32_t* ring;
+  const int64_t* state;
+  int32_t* lens_out;
+  int64_t* state_out;
+  int64_t* slots;
+  int32_t* granted;
+  int4* plan;      // [R]: ring position of the first page taken, of the first page given back, old length, new positions
+                   // granted (-1: ended)
+  int n_pages, R, max_blocks, page_log2, max_new;
+};
+
+constexpr int kPlanThreads = 1024;
+
+struct RowNeed {
+  int len, held, want;   // length, pages held, new positions asked for (negative: ended)
+  int need, give;        // pages asked for, pages given back
+  bool fits;
+};
+__device__ __forceinline__ RowNeed row_need(const PageUpdate& a, int r) {
+  const int page = 1 << a.page_log2, most = a.max_blocks << a.page_log2;
+  RowNeed n;
+  n.len = min(max(a.lens[r], 0), most);
+  n.want = a.n_new[r];
+  n.held = (n.len + page - 1) >> a.page_log2;
+  n.fits = n.want >= 0 && n.want <= most - n.len;
+  n.need = n.fits ? (int)(((long long)n.len + n.want + page - 1) >> a.page_log2) - n.held : 0;
+  n.give = n.want < 0 ? n.held : 0;
+  return n;
+}
+
+// head in [0, n_pages), free in [0, n_pages]: whatever the caller's array holds
+__device__ __forceinline__ void ring_state(const PageUpdate& a, int& head, int& free) {
+  const long long h = a.state[0] % a.n_pages, f = a.state[1];
+  head = (int)(h < 0 ? h + a.n_pages : h);
+  free = (int)(f < 0 ? 0 : (f > a.n_pages ? a.n_pages : f));
+}
+
+// position `at` + `by` of the ring; at in [0, n_pages), by >= 0
+__device__ __forceinline__ int ring_at(const PageUpdate& a, int at, long long by) {
+  const long long x = at + by;
+  return (int)(x < a.n_pages ? x : x % a.n_pages);
+}
+
+// One entry each: the table's block `held + j` of a row that takes pages, the ring's entry for block b of a row that has
+// ended, the i-th slot of a row.
+__device__ __forceinline__ void take_page(const PageUpdate& a, int r, int pop, int held, int j) {
+  a.table[(size_t)r * a.max_blocks + held + j] = a.ring[ring_at(a, pop, j)];
+}
+__device__ __forceinline__ void give_page(const PageUpdate& a, int r, int push, int b) {
+  a.ring[ring_at(a, push, b)] = a.table[(size_t)r * a.max_blocks + b];
+}
+__device__ __forceinline__ void write_slot(const PageUpdate& a, int r, int pop, int held, int len, int count, int i) {
+  long long slot = -1;
+  if (i < count) {
+    const int p = len + i, b = p >> a.page_log2;
+    // (a block that this call enters is read from the ring, not from the table: another thread enters it)
+    const int page = b >= held ? a.ring[ring_at(a, pop, b - held)] : a.table[(size_t)r * a.max_blocks + b];
+    if (page >= 0 && page < a.n_pages)
+      slot = ((long long)page << a.page_log2) + (p & ((1 << a.page_log2) - 1));
+  }
+  a.slots[(size_t)r * a.max_new + i] = slot;
+}
+
+// One workgroup: the scan over the rows.  plan[r], the new lengths, what was granted, the ring's new state.
+__global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(PageUpdate a) {
+  __shared__ int wave_need[kPlanThreads / 64], wave_give[kPlanThreads / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int head, free;
+  ring_state(a, head, free);
+  int need_before = 0, give_before = 0;   // of the rows before this round's (sums stay below R * max_blocks < 2^31)
+  int taken = 0;                          // pages granted up to here by this thread's rows
+  for (int base = 0; base < a.R; base += kPlanThreads) {
+    const int r = base + tid;
+    RowNeed n{0, 0, 0, 0, 0, false};
+    if (r < a.R) n = row_need(a, r);
+    const int need_in = wave_inclusive_sum(n.need), give_in = wave_inclusive_sum(n.give);
+    __syncthreads();
+    if (lane == 63) {
+      wave_need[wave] = need_in;
+      wave_give[wave] = give_in;
+    }
+    __syncthreads();
+    int need_to = need_before + need_in, give_to = give_before + give_in;
+#pragma unroll
+    for (int w = 0; w < kPlanThreads / 64; ++w) {
+      need_to += w < wave ? wave_need[w] : 0;
+      give_to += w < wave ? wave_give[w] : 0;
+      need_before += wave_need[w];
+      give_before += wave_give[w];
+    }
+    if (r < a.R) {
+      const bool grant = n.fits && (n.need == 0 || need_to <= free);
+      const int count = n.want < 0 ? -1 : (grant ? n.want : 0);
+      taken += grant ? n.need : 0;
+      a.plan[r] = make_int4(ring_at(a, head, grant ? need_to - n.need : 0), ring_at(a, head, (long long)free + (give_to - n.give)),
+                            n.len, count);
+      a.lens_out[r] = n.want < 0 ? 0 : n.len + count;
+      if (a.granted) a.granted[r] = count;
+    }
+  }
+  taken = wave_sum(taken);
+  __syncthreads();
+  if (lane == 0) wave_need[wave] = taken;
+  __syncthreads();
+  if (tid == 0) {
+    long long all = 0;
+    for (int w = 0; w < kPlanThreads / 64; ++w) all += wave_need[w];
+    const long long left = free - all + give_before;
+    a.state_out[0] = ring_at(a, head, all);
+    a.state_out[1] = left > a.n_pages ? a.n_pages : left;
+  }
+}
+
+// grid (R, parts): the entries of one row.
+__global__ void __launch_bounds__(256) page_fill_kernel(PageUpdate a) {
+  const int r = blockIdx.x, at = blockIdx.y * 256 + threadIdx.x, step = gridDim.y * 256;
+  const int4 plan = a.plan[r];
+  const int page = 1 << a.page_log2, len = plan.z, count = plan.w;
+  const int held = (len + page - 1) >> a.page_log2;
+  if (count < 0) {
+    for (int b = at; b < held; b += step) give_page(a, r, plan.y, b);
+  } else {
+    const int need = (int)(((long long)len + count + page - 1) >> a.page_log2) - held;
+    for (int j = at; j < need; j += step) take_page(a, r, plan.x, held, j);
+  }
+  for (int i = at; i < a.max_new; i += step) write_slot(a, r, plan.x, held, len, count, i);
+}
+
+static hipError_t launch_page_update(const PageUpdate& a, hipStream_t s) {
+  hipLaunchKernelGGL(page_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int longest = a.max_new > a.max_blocks ? a.max_new : a.max_blocks;
+  int parts = (longest + 1023) / 1024;
+  if (parts > 16) parts = 16;
+  hipLaunchKernelGGL(page_fill_kernel, dim3(a.R, parts), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace meda
+
+extern "C" {
+
+size_t meda_page_update_workspace_bytes(int32_t n_rows) {
+  if (n_rows < 1) return 0;
+  return ((size_t)n_rows * sizeof(int4) + 255) / 256 * 256;
+}
+
+meda_status meda_page_update(const meda_page_params* params, const int32_t* lens, const int32_t* n_new, int32_t* table,
+                             int32_t* free_ring, const int64_t* free_state, int32_t* lens_out, int64_t* free_state_out,
+                             int64_t* slots, int32_t* granted, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  using namespace meda;
+  if (!params) return MEDA_ERR_INVALID_ARG;
+  const meda_page_params& p = *params;
+  if (p.n_pages < 1 || p.n_rows < 1 || p.max_blocks < 1 || p.max_new < 0) return MEDA_ERR_INVALID_ARG;
+  if (p.n_pages > INT32_MAX || p.n_rows > 65536 || !valid_page_size(p.page_size)) return MEDA_ERR_UNSUPPORTED;
+  if ((int64_t)p.n_rows * p.max_blocks > INT32_MAX || (int64_t)p.max_blocks * p.page_size > INT32_MAX) return MEDA_ERR_UNSUPPORTED;
+  if (!lens || !n_new || !table || !free_ring || !free_state || !lens_out || !free_state_out) return MEDA_ERR_INVALID_ARG;
+  if (p.max_new > 0 && !slots) return MEDA_ERR_INVALID_ARG;
+  const uintptr_t words = (uintptr_t)lens | (uintptr_t)n_new | (uintptr_t)table | (uintptr_t)free_ring | (uintptr_t)lens_out | (uintptr_t)granted;
+  const uintptr_t longs = (uintptr_t)free_state | (uintptr_t)free_state_out | (uintptr_t)slots;
+  if ((words & 3u) || (longs & 7u)) return MEDA_ERR_INVALID_ARG;
+  // the same array or none of it in common
+  const intptr_t dl = (intptr_t)lens_out - (intptr_t)lens, ds = (intptr_t)free_state_out - (intptr_t)free_state;
+  const intptr_t nl = (intptr_t)p.n_rows * 4;
+  if ((dl != 0 && dl < nl && dl > -nl) || (ds != 0 && ds < 16 && ds > -16)) return MEDA_ERR_INVALID_ARG;
+  if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < meda_page_update_workspace_bytes(p.n_rows)) return MEDA_ERR_WORKSPACE;
+
+  PageUpdate a;
+  a.lens = lens; a.n_new = n_new; a.table = table; a.ring = free_ring; a.state = free_state;
+  a.lens_out = lens_out; a.state_out = free_state_out; a.slots = p.max_new > 0 ? slots : nullptr; a.granted = granted;
+  a.plan = static_cast<int4*>(workspace);
+  a.n_pages = (int)p.n_pages; a.R = p.n_rows; a.max_blocks = p.max_blocks;
+  a.page_log2 = __builtin_ctz((unsigned)p.page_size); a.max_new = p.max_new;
+  return launch_page_update(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? MEDA_OK : MEDA_ERR_HIP;
+}
+
+}  // extern "C"
