@@ -20,18 +20,31 @@ def _p(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-def _stream(stream, device):
-    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
-
-
-def _call(fn, device, *args):
-    """The library launches on the current device: the one where the tensors are."""
-    if torch.cuda.current_device() == device.index:
-        status = fn(*args)
+def _call(fn, device: int, stream, *args):
+    """Launches on the current device: the one where the tensors are."""
+    if torch._C._cuda_getDevice() == device:
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream)
     else:
         with torch.cuda.device(device):
-            status = fn(*args)
-    _check(status)
+            status = fn(*args, (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream)
+    if status != 0:
+        _check(status)
+
+
+# A call of a kind that was checked before (the same shapes, strides, types and devices) is not checked again: half of the
+# time of a small call went into it.  What an entry holds depends on nothing else, addresses least of all.
+_checked: dict = {}
+
+
+def _remember(key, entry):
+    if len(_checked) >= 1024:
+        _checked.clear()
+    _checked[key] = entry
+    return entry
+
+
+def _kind(t):
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
 
 
 def _want(name, t, shape, dtype, device):
@@ -47,13 +60,18 @@ def _want_rows(name, t, shape, dtype, device):
             or (t.numel() > 0 and t.stride(-1) != 1)):
         raise ValueError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} with contiguous rows on {device}")
     step = 16 // t.element_size()
-    if t.numel() > 0 and (t.data_ptr() % 16 or any(n > 1 and s % step for n, s in zip(t.shape[:-1], t.stride()[:-1]))):
+    if t.numel() > 0 and any(n > 1 and s % step for n, s in zip(t.shape[:-1], t.stride()[:-1])):
         raise ValueError(f"{name}: rows must start at multiples of 16 bytes")
 
 
 def _strides(t: torch.Tensor):
     """{token, head} strides; those of dimensions of one entry do not matter."""
     return (ctypes.c_int64 * 2)(t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+
+
+def _extent(t, dims):
+    """Bytes from the first element of these dimensions to behind the last."""
+    return (sum((t.shape[i] - 1) * t.stride(i) for i in dims) + 1) * t.element_size() if t.numel() else 0
 
 
 def _want_no_overlap(name, out, other_name, other, may_be_same):
@@ -64,16 +82,14 @@ def _want_no_overlap(name, out, other_name, other, may_be_same):
     if may_be_same and a == b and out.shape == other.shape and all(
             n == 1 or s == r for n, s, r in zip(out.shape, out.stride(), other.stride())):
         return
-    def extent(t, dims):   # bytes from the first element of these dimensions to behind the last
-        return (sum((t.shape[i] - 1) * t.stride(i) for i in dims) + 1) * size
-    if a + extent(out, (0, 1, 2)) <= b or b + extent(other, (0, 1, 2)) <= a:
+    if a + _extent(out, (0, 1, 2)) <= b or b + _extent(other, (0, 1, 2)) <= a:
         return
     # interleaved views of one buffer, as q and k of a fused projection: equally far apart in one dimension, and inside
     # that distance next to each other
     for i in (0, 1):
         step = out.stride(i) * size
-        if step == other.stride(i) * size and step > 0 and (b - a) % step >= extent(out, (1 - i, 2)) and (
-                (a - b) % step >= extent(other, (1 - i, 2))):
+        if step == other.stride(i) * size and step > 0 and (b - a) % step >= _extent(out, (1 - i, 2)) and (
+                (a - b) % step >= _extent(other, (1 - i, 2))):
             return
     raise ValueError(f"{name} overlaps {other_name}")
 
@@ -109,6 +125,8 @@ class PagePool:
         self.desc = MedaPagePool(n, k_pages.stride(0) if n > 1 else 0, heads, d, page, code, _p(k_pages), _p(v_pages),
                                  _p(k_scales), _p(v_scales))
         self.ref = ctypes.byref(self.desc)
+        self.index = self.device.index
+        self.key = (n, heads, page, d, code, self.index)
 
     @classmethod
     def empty(cls, n_pages, n_kv_heads, page_size, head_dim, dtype=torch.bfloat16, device="cuda:0") -> "PagePool":
@@ -136,6 +154,7 @@ class RotaryPlan:
         self.inv_freq, self.axis, self.n_axes, self.interleaved = inv_freq, axis, n_axes, interleaved
         self.rot_dim, self.device = 2 * inv_freq.numel(), inv_freq.device
         self.flags = ROTARY_INTERLEAVED if interleaved else 0
+        self.key = (self.rot_dim, n_axes, axis is None, interleaved, self.device.index)
 
     def _positions(self, positions, n_tokens, device):
         """The stride from one axis' positions to the next."""
@@ -159,36 +178,58 @@ def meda_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Ten
     """Rotary positions of q [T][Hq][d] and k [T][Hk][d] (any strides with contiguous rows; ``x.transpose(0, 1)`` of an
     [H][T][d] array is such a view).  The outputs may be the inputs; without them new ones are made.  ``inverse`` turns
     back: the gradient of the rotation."""
-    if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.dtype not in _DTYPES or not q.is_cuda:
+    key = ("rotary", _kind(q), _kind(k), _kind(positions), None if rope is None else rope.key, _kind(q_out), _kind(k_out), inverse)
+    plan = _checked.get(key)
+    if plan is None:
+        plan = _remember(key, _plan_rotary(q, k, positions, rope, q_out, k_out, inverse))
+    params, dev, new_q, new_k, ext = plan
+    if new_q is not None:
+        q_out = torch.empty(new_q, dtype=q.dtype, device=q.device)
+    if new_k is not None:
+        k_out = torch.empty(new_k, dtype=k.dtype, device=k.device)
+    pq, pk, po, pko = q.data_ptr(), _p(k), q_out.data_ptr(), _p(k_out)
+    for name, out, a, n in (("q_out", q_out, po, ext[2]), ("k_out", k_out, pko, ext[3])):
+        if out is not None:
+            if a < pq + ext[0] and pq < a + n:
+                _want_no_overlap(name, out, "q", q, name == "q_out")
+            if pk is not None and a < pk + ext[1] and pk < a + n:
+                _want_no_overlap(name, out, "k", k, name == "k_out")
+    if pko is not None and po < pko + ext[3] and pko < po + ext[2]:
+        _want_no_overlap("q_out", q_out, "k_out", k_out, False)
+    _call(load_library().meda_rotary, dev, stream, params, pq, pk, positions.data_ptr(), rope.inv_freq.data_ptr(), _p(rope.axis), po, pko)
+    return q_out, k_out
+
+
+def _plan_rotary(q, k, positions, rope, q_out, k_out, inverse):
+    """The checks of a call, its parameters, the shapes of the outputs to make, and the extents of q, k and the outputs."""
+    if q.dim() != 3 or q.dtype not in _DTYPES or not q.is_cuda:
         raise ValueError("q: expected a float32 or bfloat16 tensor [tokens][heads][head_dim] on the GPU")
     T, Hq, d = q.shape
-    if rope.rot_dim > d:
-        raise ValueError(f"the plan turns {rope.rot_dim} elements, a row has {d}")
+    if rope is None or rope.rot_dim > d:
+        raise ValueError("a plan of the rotation is needed" if rope is None else f"the plan turns {rope.rot_dim} elements, a row has {d}")
     dt, dev = q.dtype, q.device
     _want_rows("q", q, (T, Hq, d), dt, dev)
-    q_out = torch.empty((T, Hq, d), dtype=dt, device=dev) if q_out is None else q_out
-    _want_rows("q_out", q_out, (T, Hq, d), dt, dev)
-    _want_no_overlap("q_out", q_out, "q", q, True)
-    Hk = 0
-    zero = (ctypes.c_int64 * 2)(0, 0)
-    ks = ko = zero
+    if q_out is not None:
+        _want_rows("q_out", q_out, (T, Hq, d), dt, dev)
+    qo = _strides(q_out) if q_out is not None else (ctypes.c_int64 * 2)(Hq * d, d)
+    Hk, ks, ko = 0, (ctypes.c_int64 * 2)(0, 0), (ctypes.c_int64 * 2)(0, 0)
     if k is not None:
         if k.dim() != 3:
             raise ValueError("k: expected [tokens][heads][head_dim]")
         Hk = k.shape[1]
         _want_rows("k", k, (T, Hk, d), dt, dev)
-        k_out = torch.empty((T, Hk, d), dtype=dt, device=dev) if k_out is None else k_out
-        _want_rows("k_out", k_out, (T, Hk, d), dt, dev)
-        _want_no_overlap("k_out", k_out, "k", k, True)
-        for name, out in (("q_out", q_out), ("k_out", k_out)):
-            _want_no_overlap(name, out, "the other input", k if name == "q_out" else q, False)
-        ks, ko = _strides(k), _strides(k_out)
+        if k_out is not None:
+            _want_rows("k_out", k_out, (T, Hk, d), dt, dev)
+        ks, ko = _strides(k), (_strides(k_out) if k_out is not None else (ctypes.c_int64 * 2)(Hk * d, d))
     elif k_out is not None:
         raise ValueError("k_out without k")
-    params = MedaRotaryParams(T, _strides(q), _strides(q_out), ks, ko, rope._positions(positions, T, dev), Hq, Hk, d,
-                              rope.rot_dim, rope.n_axes, _DTYPES[dt], rope.flags | (ROTARY_INVERSE if inverse else 0))
-    _call(load_library().meda_rotary, dev, ctypes.byref(params), _p(q), _p(k), _p(positions), _p(rope.inv_freq), _p(rope.axis), _p(q_out), _p(k_out), _stream(stream, dev))
-    return q_out, k_out
+    params = MedaRotaryParams(T, _strides(q), qo, ks, ko, rope._positions(positions, T, dev), Hq, Hk, d, rope.rot_dim, rope.n_axes,
+                              _DTYPES[dt], rope.flags | (ROTARY_INVERSE if inverse else 0))
+    size, dims = q.element_size(), (0, 1, 2)
+    ext = (_extent(q, dims), 0 if k is None else _extent(k, dims), T * Hq * d * size if q_out is None else _extent(q_out, dims),
+           0 if k is None else (T * Hk * d * size if k_out is None else _extent(k_out, dims)))
+    return (ctypes.byref(params), dev.index, (T, Hq, d) if q_out is None else None,
+            (T, Hk, d) if k is not None and k_out is None else None, ext)
 
 
 def meda_paged_append(pool: PagePool, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor,
@@ -197,6 +238,26 @@ def meda_paged_append(pool: PagePool, k: torch.Tensor, v: torch.Tensor, slots: t
                       stream=None) -> Optional[torch.Tensor]:
     """Writes k, v [M][Hkv][d] of new tokens to their ``slots`` (int64 [M], -1: none), k rotated where a plan is given;
     returns q [M][Hq][d] rotated alike (``q_out``, which may be q)."""
+    key = ("append", pool.key, _kind(k), _kind(v), _kind(slots), _kind(q), _kind(positions), None if rope is None else rope.key, _kind(q_out))
+    plan = _checked.get(key)
+    if plan is None:
+        plan = _remember(key, _plan_append(pool, k, v, slots, q, positions, rope, q_out))
+    params, new_q, ext = plan
+    if new_q is not None:
+        q_out = torch.empty(new_q, dtype=q.dtype, device=q.device)
+    po = _p(q_out)
+    if po is not None:
+        for name, t, n in (("q", q, ext[0]), ("k", k, ext[1]), ("v", v, ext[2])):
+            a = t.data_ptr()
+            if po < a + n and a < po + ext[3]:
+                _want_no_overlap("q_out", q_out, name, t, name == "q")
+    turn = (None, None, None) if rope is None else (positions.data_ptr(), rope.inv_freq.data_ptr(), _p(rope.axis))
+    _call(load_library().meda_paged_append, pool.index, stream, pool.ref, params, _p(q), k.data_ptr(), v.data_ptr(), *turn, slots.data_ptr(), po)
+    return q_out
+
+
+def _plan_append(pool, k, v, slots, q, positions, rope, q_out):
+    """The checks of a call, its parameters, the shape of the output to make, and the extents of q, k, v and the output."""
     dev, dt, d = pool.device, pool.row_dtype, pool.head_dim
     if slots.dim() != 1 or slots.dtype != torch.int64 or slots.device != dev:
         raise ValueError(f"slots: expected an int64 vector on {dev}")
@@ -212,13 +273,9 @@ def meda_paged_append(pool: PagePool, k: torch.Tensor, v: torch.Tensor, slots: t
             raise ValueError("q: expected [tokens][heads][head_dim]")
         Hq = q.shape[1]
         _want_rows("q", q, (M, Hq, d), dt, dev)
-        q_out = torch.empty((M, Hq, d), dtype=dt, device=dev) if q_out is None else q_out
-        _want_rows("q_out", q_out, (M, Hq, d), dt, dev)
-        _want_no_overlap("q_out", q_out, "q", q, True)
-        for name, t in (("k", k), ("v", v)):
-            if q_out.data_ptr() != q.data_ptr():
-                _want_no_overlap("q_out", q_out, name, t, False)
-        qs, qo = _strides(q), _strides(q_out)
+        if q_out is not None:
+            _want_rows("q_out", q_out, (M, Hq, d), dt, dev)
+        qs, qo = _strides(q), (_strides(q_out) if q_out is not None else (ctypes.c_int64 * 2)(Hq * d, d))
     elif q_out is not None:
         raise ValueError("q_out without q")
     rot, axes, flags, pos_stride = 0, 1, 0, 0
@@ -230,8 +287,10 @@ def meda_paged_append(pool: PagePool, k: torch.Tensor, v: torch.Tensor, slots: t
         raise ValueError("positions without a plan of the rotation")
     params = MedaAppendParams(M, qs, qo, _strides(k), _strides(v), pos_stride, slots.stride(0) if M > 1 else 1, Hq, rot, axes,
                               _DTYPES[dt], flags)
-    _call(load_library().meda_paged_append, dev, pool.ref, ctypes.byref(params), _p(q), _p(k), _p(v), _p(positions) if rope is not None else None, _p(rope.inv_freq) if rope is not None else None, _p(rope.axis) if rope is not None else None, _p(slots), _p(q_out), _stream(stream, dev))
-    return q_out
+    dims = (0, 1, 2)
+    ext = (0 if q is None else _extent(q, dims), _extent(k, dims), _extent(v, dims),
+           0 if q is None else (M * Hq * d * k.element_size() if q_out is None else _extent(q_out, dims)))
+    return ctypes.byref(params), (M, Hq, d) if q is not None and q_out is None else None, ext
 
 
 def _want_table(table, lens, device):
@@ -250,7 +309,19 @@ def _want_table(table, lens, device):
 def meda_paged_store(pool: PagePool, cache: CompressedCache, table: torch.Tensor, lens: torch.Tensor, stream=None) -> None:
     """Moves the caches that a call of meda_compress returned to pages: row n * L + l of ``table`` and ``lens`` (the lengths
     that meda_page_update granted) belongs to layer l of sequence n."""
+    key = ("store", pool.key, cache.n_kv_heads, _kind(cache.k_out), _kind(cache.v_out), _kind(cache.layer_len), _kind(cache.layer_off),
+           _kind(table), _kind(lens))
+    params = _checked.get(key)
+    if params is None:
+        params = _remember(key, _plan_store(pool, cache, table, lens))
+    _call(load_library().meda_paged_store, pool.index, stream, pool.ref, params, cache.k_out.data_ptr(), cache.v_out.data_ptr(),
+          cache.layer_len.data_ptr(), cache.layer_off.data_ptr(), lens.data_ptr(), table.data_ptr())
+
+
+def _plan_store(pool, cache, table, lens):
     dev, dt, d = pool.device, pool.row_dtype, pool.head_dim
+    if cache.layer_len.dim() not in (1, 2):
+        raise ValueError("layer_len: expected [layers] or [sequences][layers]")
     N, L = (1, cache.layer_len.shape[0]) if cache.layer_len.dim() == 1 else cache.layer_len.shape
     batch = () if cache.layer_len.dim() == 1 else (N,)
     _want("layer_len", cache.layer_len, batch + (L,), torch.int32, dev)
@@ -263,8 +334,7 @@ def meda_paged_store(pool: PagePool, cache: CompressedCache, table: torch.Tensor
     R, blocks, ts, ls = _want_table(table, lens, dev)
     if R != N * L:
         raise ValueError(f"table: expected {N * L} rows, one per sequence and layer")
-    params = MedaStoreParams(rows, ts, ls, N, L, blocks, _DTYPES[dt])
-    _call(load_library().meda_paged_store, dev, pool.ref, ctypes.byref(params), _p(cache.k_out), _p(cache.v_out), _p(cache.layer_len), _p(cache.layer_off), _p(lens), _p(table), _stream(stream, dev))
+    return ctypes.byref(MedaStoreParams(rows, ts, ls, N, L, blocks, _DTYPES[dt]))
 
 
 class PagedDecoder:
@@ -278,33 +348,43 @@ class PagedDecoder:
         if need == 0:
             raise MedaError(1, "invalid or unsupported parameters of the paged step")
         self.dtype = dt
-        self.workspace = torch.empty(need, dtype=torch.uint8, device=pool.device)
+        self.workspace, self._workspace_bytes = torch.empty(need, dtype=torch.uint8, device=pool.device), need
+        self._calls: dict = {}     # parameters of calls by the shapes and strides of their tensors, as in _checked
         self.out = torch.empty((n_rows, n_q_heads, pool.head_dim), dtype=dt, device=pool.device)
 
     def __call__(self, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, out: Optional[torch.Tensor] = None,
                  stream=None) -> torch.Tensor:
         """q [rows][Hq][d] (rows any distance apart) over the pages of ``table`` [rows][blocks]; ``lens`` [rows].  Without
         ``out`` the result lies in a buffer that the next call overwrites."""
-        pool, shape = self.pool, (self.n_rows, self.n_q_heads, self.pool.head_dim)
-        dev = pool.device
         out = self.out if out is None else out
+        key = (_kind(q), _kind(table), _kind(lens), _kind(out))
+        call = self._calls.get(key)
+        if call is None:
+            if len(self._calls) >= 64:
+                self._calls.clear()
+            call = self._calls[key] = self._plan(q, table, lens, out)
+        if out is not self.out:
+            _want_no_overlap("out", out, "q", q, False)
+        pool = self.pool
+        _call(load_library().meda_paged_attention, pool.index, stream, pool.ref, call, q.data_ptr(), table.data_ptr(), lens.data_ptr(),
+              out.data_ptr(), self.workspace.data_ptr(), self._workspace_bytes)
+        return out
+
+    def _plan(self, q, table, lens, out):
+        """The checks of a call and its parameters."""
+        pool, shape = self.pool, (self.n_rows, self.n_q_heads, self.pool.head_dim)
         for name, t in (("q", q), ("out", out)):
-            _want_rows(name, t, shape, self.dtype, dev)
+            _want_rows(name, t, shape, self.dtype, pool.device)
             if shape[1] > 1 and t.stride(1) != shape[2]:
                 raise ValueError(f"{name}: the heads of a row must be contiguous")
             if shape[0] > 1 and t.stride(0) < shape[1] * shape[2]:
                 raise ValueError(f"{name}: rows must lie apart")
-        if out is not self.out:
-            _want_no_overlap("out", out, "q", q, False)
-        R, blocks, ts, ls = _want_table(table, lens, dev)
+        R, blocks, ts, ls = _want_table(table, lens, pool.device)
         if R != self.n_rows or blocks != self.max_blocks:
             raise ValueError(f"table: expected {self.n_rows} rows of {self.max_blocks} blocks")
-        p = self.params
-        row = shape[1] * shape[2]
-        call = MedaPagedParams(q.stride(0) if R > 1 else row, out.stride(0) if R > 1 else row, ts, ls, R, shape[1], blocks,
-                               p.dtype, p.softmax_scale)
-        _call(load_library().meda_paged_attention, dev, pool.ref, ctypes.byref(call), _p(q), _p(table), _p(lens), _p(out), _p(self.workspace), self.workspace.numel(), _stream(stream, dev))
-        return out
+        p, row = self.params, shape[1] * shape[2]
+        return ctypes.byref(MedaPagedParams(q.stride(0) if R > 1 else row, out.stride(0) if R > 1 else row, ts, ls, R, shape[1],
+                                            blocks, p.dtype, p.softmax_scale))
 
 
 def meda_page_update_workspace_bytes(n_rows: int) -> int:
@@ -318,6 +398,24 @@ def meda_page_update(lens: torch.Tensor, n_new: torch.Tensor, table: torch.Tenso
     """Room for ``n_new`` positions per row (negative: the row has ended), from the free pages.  ``table`` [R][blocks] and
     ``free_ring`` [n_pages] are updated in place, lens [R] and free_state [2] too unless outputs for them are given;
     ``slots`` [R][max_new] and ``granted`` [R] receive the slots and what each row got."""
+    lens_out = lens if lens_out is None else lens_out
+    free_state_out = free_state if free_state_out is None else free_state_out
+    key = ("pages", _kind(lens), _kind(n_new), _kind(table), _kind(free_ring), _kind(free_state), page_size, _kind(lens_out),
+           _kind(free_state_out), _kind(slots), _kind(granted), _kind(workspace))
+    plan = _checked.get(key)
+    if plan is None:
+        plan = _remember(key, _plan_update(lens, n_new, table, free_ring, free_state, page_size, lens_out, free_state_out, slots, granted,
+                                           workspace))
+    params, dev, max_new, need = plan
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=table.device)
+    _call(load_library().meda_page_update, dev, stream, params, lens.data_ptr(), n_new.data_ptr(), table.data_ptr(), free_ring.data_ptr(),
+          free_state.data_ptr(), lens_out.data_ptr(), free_state_out.data_ptr(), slots.data_ptr() if max_new else None, _p(granted),
+          workspace.data_ptr(), workspace.shape[0])
+
+
+def _plan_update(lens, n_new, table, free_ring, free_state, page_size, lens_out, free_state_out, slots, granted, workspace):
+    """The checks of a call, its parameters, the columns of slots, the workspace's size."""
     dev = table.device
     if not table.is_cuda:
         raise ValueError("table: expected a tensor on the GPU")
@@ -326,8 +424,6 @@ def meda_page_update(lens: torch.Tensor, n_new: torch.Tensor, table: torch.Tenso
     R, blocks = table.shape
     if page_size not in PAGE_SIZES:
         raise ValueError(f"page_size {page_size}: expected one of {PAGE_SIZES}")
-    lens_out = lens if lens_out is None else lens_out
-    free_state_out = free_state if free_state_out is None else free_state_out
     for name, t, shape, dtype in (("lens", lens, (R,), torch.int32), ("n_new", n_new, (R,), torch.int32),
                                   ("table", table, (R, blocks), torch.int32), ("lens_out", lens_out, (R,), torch.int32),
                                   ("free_state", free_state, (2,), torch.int64),
@@ -344,12 +440,11 @@ def meda_page_update(lens: torch.Tensor, n_new: torch.Tensor, table: torch.Tenso
         _want("slots", slots, (R, max_new), torch.int64, dev)
     if granted is not None:
         _want("granted", granted, (R,), torch.int32, dev)
-    if workspace is None:
-        workspace = torch.empty(meda_page_update_workspace_bytes(R), dtype=torch.uint8, device=dev)
-    elif workspace.device != dev or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
-        raise ValueError(f"workspace: expected a contiguous uint8 tensor on {dev}")
-    params = MedaPageParams(free_ring.shape[0], R, blocks, page_size, max_new)
-    _call(load_library().meda_page_update, dev, ctypes.byref(params), _p(lens), _p(n_new), _p(table), _p(free_ring), _p(free_state), _p(lens_out), _p(free_state_out), _p(slots) if max_new else None, _p(granted), _p(workspace), workspace.numel(), _stream(stream, dev))
+    if workspace is not None and (workspace.dim() != 1 or workspace.device != dev or workspace.dtype != torch.uint8
+                                  or not workspace.is_contiguous()):
+        raise ValueError(f"workspace: expected a contiguous uint8 vector on {dev}")
+    return (ctypes.byref(MedaPageParams(free_ring.shape[0], R, blocks, page_size, max_new)), dev.index, max_new,
+            meda_page_update_workspace_bytes(R))
 
 
 class PagedCache:

@@ -74,62 +74,74 @@ __device__ __forceinline__ long long uniform(long long v) {
   return (long long)(((unsigned long long)hi << 32) | lo);
 }
 
-// Inclusive sum over a workgroup of kLocateThreads threads; `total` is the sum of all.  Needs 4 entries of LDS, which are
-// free again after the next barrier.
-__device__ __forceinline__ long long group_inclusive_sum(long long v, long long* lds, long long& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const long long up = __shfl_up(v, o, kWave);
-    if (lane >= o) v += up;
-  }
-  if (lane == 63) lds[wave] = v;
-  __syncthreads();
-  total = 0;
-  long long before = 0;
-#pragma unroll
-  for (int w = 0; w < kLocateThreads / 64; ++w) {
-    before += w < wave ? lds[w] : 0;
-    total += lds[w];
-  }
-  total = uniform(total);
-  return v + before;
-}
-
 struct RowOfUnit {
   int row;          // -1: no unit at all
+  int size;         // units of the row, per head
   long long first;  // number of the row's first unit
 };
 
-// Rows 0 .. R-1 of units(r) >= 0 units each, numbered row after row: finds the row of unit number pick(total), which every
-// thread of the workgroup (kLocateThreads threads) receives.  Every thread adds up the same number of consecutive rows.
-// pick sees the total and must give a number below it, or a negative one for nothing.
+// Rows 0 .. R-1 of units(r) >= 0 units in each of Hkv heads, numbered row after row and head after head: finds the row of
+// unit number pick(total), as the same value in every thread of a workgroup of kLocateThreads.  pick sees the total and must
+// give a number below it, or a negative one for nothing.
+//
+// Up to 64 rows: every wave searches on its own, a lane per row (all workgroups of a launch begin with this, and the data's
+// latency is all it should cost).  More: every thread adds up the same number of consecutive rows, with two barriers.
 template <typename Units, typename Pick>
-__device__ __forceinline__ RowOfUnit locate_row(int R, Units units, Pick pick) {
+__device__ __forceinline__ RowOfUnit locate_row(int R, int Hkv, Units units, Pick pick) {
+  const int lane = threadIdx.x & 63;
+  if (R <= 64) {
+    const int mine = lane < R ? units(lane) : 0;
+    // (64 rows of at most 2^25 units each: the sum fits 32 bits)
+    const unsigned end = (unsigned)wave_inclusive_sum(mine);
+    const long long total = (long long)(unsigned)__builtin_amdgcn_readlane((int)end, 63) * Hkv;
+    const long long unit = pick(total);
+    RowOfUnit out{-1, 0, 0};
+    const unsigned long long b = __ballot(unit >= (long long)(end - (unsigned)mine) * Hkv && unit < (long long)end * Hkv);
+    if (unit >= 0 && b != 0ull) {
+      out.row = __ffsll(b) - 1;
+      out.size = __builtin_amdgcn_readlane(mine, out.row);
+      out.first = (long long)(unsigned)__builtin_amdgcn_readlane((int)(end - (unsigned)mine), out.row) * Hkv;
+    }
+    return out;
+  }
   __shared__ long long sums[kLocateThreads / 64];
   __shared__ RowOfUnit found;
+  const int wave = threadIdx.x >> 6;
   const int per = (R + kLocateThreads - 1) / kLocateThreads;
   const int r0 = min((int)threadIdx.x * per, R), r1 = min(r0 + per, R);
   long long mine = 0;
   for (int r = r0; r < r1; ++r) mine += units(r);
-  long long total;
-  const long long end = group_inclusive_sum(mine, sums, total);
-  const long long unit = pick(total);
-  if (threadIdx.x == 0) found = RowOfUnit{-1, 0};
+  long long end = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const long long up = __shfl_up(end, o, kWave);
+    if (lane >= o) end += up;
+  }
+  if (lane == 63) sums[wave] = end;
+  if (threadIdx.x == 0) found = RowOfUnit{-1, 0, 0};
   __syncthreads();
-  if (unit >= end - mine && unit < end) {
+  long long total = 0;
+#pragma unroll
+  for (int w = 0; w < kLocateThreads / 64; ++w) {
+    end += w < wave ? sums[w] : 0;
+    total += sums[w];
+  }
+  const long long unit = pick(uniform(total) * Hkv);
+  if (unit >= (end - mine) * Hkv && unit < end * Hkv) {
     long long at = end - mine;
-    int r = r0;
-    for (; r < r1 - 1; ++r) {
-      const long long n = units(r);
-      if (unit < at + n) break;
+    for (int r = r0; r < r1; ++r) {
+      const int n = units(r);
+      if (unit < (at + n) * Hkv) {
+        found = RowOfUnit{r, n, at * Hkv};
+        break;
+      }
       at += n;
     }
-    found = RowOfUnit{r, at};
   }
   __syncthreads();
   RowOfUnit out;
   out.row = __builtin_amdgcn_readfirstlane(found.row);
+  out.size = __builtin_amdgcn_readfirstlane(found.size);
   out.first = uniform(found.first);
   return out;
 }

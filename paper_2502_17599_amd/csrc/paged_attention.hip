@@ -21,8 +21,16 @@ namespace meda {
 constexpr int kAttThreads = kLocateThreads, kAttWaves = kAttThreads / 64;
 constexpr int kUnit = 32;         // positions: a step of one wave
 constexpr int kMinUnits = 4;      // a workgroup's share, at least: a step per wave
-constexpr int kAttGroups = 768;   // workgroups: three per CU
 constexpr int kMaxGroup = 16;     // query heads per kv head
+// Workgroups per CU, and waves per SIMD, as many as the registers allow.  All workgroups of a launch are at work at once,
+// each on one share, and every CU has equally many of them: 512 workgroups of which three fit a CU were spread unevenly
+// (64 requests, 435 MB: 95 us against 86 with 768), and with two or three rounds of shorter shares the workgroups' searches
+// and the joins cost more than the evener end gained (104 and 111 us against 99, before the pages of 32 steps were loaded
+// at once).
+constexpr int groups_per_cu(int q_bytes, int d, int gp) {
+  return q_bytes == 4 ? (gp <= 2 ? 4 : (gp <= 8 ? 3 : 2)) : (d == 64 ? 4 : 3);
+}
+constexpr int kCus = 256;
 
 struct PagedArgs {
   Pool pool;
@@ -30,7 +38,8 @@ struct PagedArgs {
   char* out;
   const int32_t* table;
   const int32_t* lens;
-  float* part;             // [2 * groups][G][d + 2]: value sum, maximum (base-2 logits), normaliser
+  float* part;             // [2 * groups][G][d]: value sums of the pieces
+  float2* part_mz;         // [2 * groups][G]: their maximum (base-2 logits) and normaliser
   int2* cut;               // [groups]: the (row, kv head) that begins in the share and goes on behind it, as
                            // (row * Hkv + head, shares it reaches into); (0, 0): none
   long long q_stride, out_stride;   // bytes
@@ -43,21 +52,29 @@ __device__ __forceinline__ int row_len(const PagedArgs& a, int r) {
   return min(max(a.lens[r * a.len_stride], 0), a.max_blocks << a.pool.page_log2);
 }
 
-// The pages of a unit's two blocks of 16 positions, as byte offsets of (page, head, place) and scale indexes.
+// The pages of the units u, u + kAttWaves, .. of a wave (32 of them, two blocks of 16 positions each): lane 2 i + b holds
+// that of block b of the i-th.  One load for 32 steps: a load of its own in every step would have to be waited for, and with
+// it, as loads come back in order, for all rows that are on their way (64 requests, 435 MB: 95 us against 81).
+__device__ __forceinline__ int load_pages(const PagedArgs& a, const int32_t* table, int u, int u1, int len) {
+  const int lane = threadIdx.x & 63;
+  const int pos = min(u + kAttWaves * (lane >> 1), u1 - 1) * kUnit;     // (units past the share repeat its last one)
+  const int p = pos + 16 * (lane & 1);
+  return table[(p < len ? p : pos) >> a.pool.page_log2];                // a block behind the end repeats the first one
+}
+
+// Where a unit's two blocks of 16 positions lie, as byte offsets of (page, head, place) and scale indexes.
 struct UnitPages {
   size_t at[2];
   size_t scale[2];
   bool ok[2];      // the page exists
 };
 template <int ROW_BYTES>
-__device__ __forceinline__ UnitPages unit_pages(const PagedArgs& a, const int32_t* table, int head, int pos, int end) {
+__device__ __forceinline__ UnitPages unit_pages(const PagedArgs& a, int pages, int step, int head, int pos, int len) {
   UnitPages u;
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
-    const int p = pos + 16 * b;
-    // a block behind the end repeats the first one
-    const int q = p < end ? p : pos;
-    const int page = __builtin_amdgcn_readfirstlane(table[q >> a.pool.page_log2]);
+    const int p = pos + 16 * b, q = p < len ? p : pos;
+    const int page = __builtin_amdgcn_readlane(pages, 2 * (step & 31) + b);
     u.ok[b] = page >= 0 && page < a.pool.n_pages;
     const size_t safe = u.ok[b] ? page : 0;
     const size_t place = ((size_t)head << a.pool.page_log2) + (q & ((1 << a.pool.page_log2) - 1));
@@ -109,7 +126,7 @@ __device__ __forceinline__ void attend_units(AttState<D>& st, const uint4 (&qp)[
       const char* src = a.pool.k + up.at[b] + (unsigned)((MASKED ? min(c, top) : c) * kRowBytes + 16 * g);
 #pragma unroll
       for (int k = 0; k < KL; ++k) {
-        const uint4 x = *reinterpret_cast<const uint4*>(src + 64 * k);
+        const uint4 x = load16_stream(src + 64 * k);
         t.k[b][k][0] = x.x; t.k[b][k][1] = x.y; t.k[b][k][2] = x.z; t.k[b][k][3] = x.w;
       }
     }
@@ -225,21 +242,25 @@ __device__ __forceinline__ void attend_units(AttState<D>& st, const uint4 (&qp)[
     }
   };
 
-  int u = u0 + wave;
+  int u = u0 + wave, step = 0;
   if (u >= u1) return;
+  auto full = [&](const UnitPages& up, int pos) { return pos + kUnit <= len && up.ok[0] && up.ok[1]; };
+  int pages = load_pages(a, table, u, u1, len), pages_behind = pages;
+  UnitPages up = unit_pages<kRowBytes>(a, pages, step, head, u * kUnit, len);
+  bool fast = full(up, u * kUnit);
   Unit rows;
   float t[8];
-  auto full = [&](const UnitPages& up, int pos) { return pos + kUnit <= len && up.ok[0] && up.ok[1]; };
-  UnitPages up = unit_pages<kRowBytes>(a, table, head, u * kUnit, len);
-  bool fast = full(up, u * kUnit);
   if (fast) load_keys(rows, up, 0, std::false_type());
   while (fast) {
     load_values(rows, up, 0, std::false_type());
     const UnitPages cur = up;
     u += kAttWaves;
+    ++step;
     fast = u < u1;
+    if ((step & 31) == 16) pages_behind = load_pages(a, table, u + 16 * kAttWaves, u1, len);
+    if ((step & 31) == 0) pages = pages_behind;
     if (fast) {
-      up = unit_pages<kRowBytes>(a, table, head, u * kUnit, len);
+      up = unit_pages<kRowBytes>(a, pages, step, head, u * kUnit, len);
       fast = full(up, u * kUnit);
     }
     logits(rows, t);
@@ -247,7 +268,7 @@ __device__ __forceinline__ void attend_units(AttState<D>& st, const uint4 (&qp)[
     finish(rows, cur, 0, t, std::false_type());
   }
   for (; u < u1; u += kAttWaves) {   // the last unit of a row; units behind a missing page
-    up = unit_pages<kRowBytes>(a, table, head, u * kUnit, len);
+    up = unit_pages<kRowBytes>(a, load_pages(a, table, u, u1, len), 0, head, u * kUnit, len);
     load_keys(rows, up, u * kUnit, std::true_type());
     logits(rows, t);
     load_values(rows, up, u * kUnit, std::true_type());
@@ -277,12 +298,9 @@ __device__ __forceinline__ void write_piece(const PagedArgs& a, bool whole, int 
       // (no weight at all, as where every page is missing: zeros)
       store_elem(a.out + r * a.out_stride + ((size_t)(head * a.G + h) * D + j) * sizeof(T), zs == 0.f ? 0.f : os / zs, T{});
     } else {
-      float* dst = a.part + ((size_t)slot * a.G + h) * (D + 2);
-      dst[j] = os;
-      if (j == 0) {
-        dst[D] = mn;
-        dst[D + 1] = zs;
-      }
+      const size_t at = (size_t)slot * a.G + h;
+      a.part[at * D + j] = os;
+      if (j == 0) a.part_mz[at] = make_float2(mn, zs);
     }
   }
 }
@@ -294,7 +312,10 @@ __device__ __forceinline__ void write_piece(const PagedArgs& a, bool whole, int 
 template <int D, int GP>
 __device__ __forceinline__ void attend_f32(const PagedArgs& a, int r, int head, const int32_t* table, int u0, int u1, int len,
                                            float (&red_o)[GP][D], float (&red_m)[GP], float (&red_z)[GP]) {
-  constexpr int LPR = D / 4, MS = 64 / LPR, E = 4, U = 2, kRowBytes = D * 4;
+  // U steps' rows are on their way while U others are worked on (fewer where the heads need the registers)
+  constexpr int LPR = D / 4, MS = 64 / LPR, E = 4, U = GP <= 4 ? 4 : 2, kRowBytes = D * 4;
+  constexpr int kRows = U * MS, kParts = kUnit / kRows;   // positions of one part of a unit; a part lies in one block
+  static_assert(kRows <= 16, "a part lies in one page");
   const int lane = threadIdx.x & 63, sub = lane / LPR, cc = lane - sub * LPR;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint4 qp[GP];
@@ -308,57 +329,80 @@ __device__ __forceinline__ void attend_f32(const PagedArgs& a, int r, int head, 
 #pragma unroll
     for (int e = 0; e < E; ++e) o[h][e] = 0.f;
 
-  for (int u = u0 + wave; u < u1; u += kAttWaves) {
-    const int pos = u * kUnit;
-    const UnitPages up = unit_pages<kRowBytes>(a, table, head, pos, len);
+  struct Part {
+    uint4 k[U], v[U];
+    int n;           // its positions: fewer than kRows at the end, none in a page that does not exist
+  };
+  auto load = [&](Part& t, int pages, int step, int u, int part) {
+    const int pos = u * kUnit + part * kRows;
+    const int page = __builtin_amdgcn_readlane(pages, 2 * (step & 31) + part * kRows / 16);
+    const bool ok = page >= 0 && page < a.pool.n_pages;
+    t.n = ok ? min(max(len - pos, 0), kRows) : 0;
+    const size_t place = ((size_t)head << a.pool.page_log2) + (pos & ((1 << a.pool.page_log2) - 1));
+    const size_t at = (size_t)(ok ? page : 0) * a.pool.page_bytes + place * kRowBytes;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int n = up.ok[b] ? min(len - pos - 16 * b, 16) : 0;   // positions of this block
-      if (n <= 0) continue;
-      const char *kb = a.pool.k + up.at[b] + cc * 16, *vb = a.pool.v + up.at[b] + cc * 16;
-      for (int i0 = 0; i0 < n; i0 += U * MS) {
-        uint4 kv[U], vv[U];
-        bool ok[U];
+    for (int w = 0; w < U; ++w) {
+      const unsigned ro = (unsigned)(min(w * MS + sub, max(t.n - 1, 0)) * kRowBytes + cc * 16);
+      t.k[w] = load16_stream(a.pool.k + at + ro);
+      t.v[w] = load16_stream(a.pool.v + at + ro);
+    }
+  };
+  auto compute = [&](const Part& t) {
 #pragma unroll
-        for (int w = 0; w < U; ++w) {
-          const int i = i0 + w * MS + sub;
-          ok[w] = i < n;
-          const unsigned ro = (unsigned)(min(i, n - 1) * kRowBytes);
-          kv[w] = load16_stream(kb + ro);
-          vv[w] = load16_stream(vb + ro);
-        }
+    for (int w = 0; w < U; ++w) {
+      const bool ok = w * MS + sub < t.n;
+      float s[GP];
 #pragma unroll
-        for (int w = 0; w < U; ++w) {
-          float s[GP];
+      for (int h = 0; h < GP; ++h) s[h] = dot4(qp[h], t.k[w]);
+      row_reduce_scatter<GP, LPR>(s, cc);
+      const float s1 = ok ? s[0] * a.scale_log2 : -INFINITY;
+      if (__ballot(s1 > m1) != 0ull) {  // a new maximum of some head in some lane group (rare after the first rows)
+        const float mn = fmaxf(m1, s1);
+        const float c1 = __builtin_amdgcn_exp2f(m1 - mn);
+        z1 *= c1;
+        m1 = mn;
+        float c[GP];
+        row_all_gather<GP, LPR>(c1, c, cc);
 #pragma unroll
-          for (int h = 0; h < GP; ++h) s[h] = dot4(qp[h], kv[w]);
-          row_reduce_scatter<GP, LPR>(s, cc);
-          const float s1 = ok[w] ? s[0] * a.scale_log2 : -INFINITY;
-          if (__ballot(s1 > m1) != 0ull) {  // a new maximum of some head in some lane group (rare after the first rows)
-            const float mn = fmaxf(m1, s1);
-            const float c1 = __builtin_amdgcn_exp2f(m1 - mn);
-            z1 *= c1;
-            m1 = mn;
-            float c[GP];
-            row_all_gather<GP, LPR>(c1, c, cc);
+        for (int h = 0; h < GP; ++h)
 #pragma unroll
-            for (int h = 0; h < GP; ++h)
-#pragma unroll
-              for (int e = 0; e < E; ++e) o[h][e] *= c[h];
-          }
-          const float p1 = ok[w] ? __builtin_amdgcn_exp2f(s1 - m1) : 0.f;
-          z1 += p1;
-          float p[GP], vf[E];
-          row_all_gather<GP, LPR>(p1, p, cc);
-          unpack4(vv[w], vf);
-#pragma unroll
-          for (int e = 0; e < E; ++e) vf[e] = ok[w] ? vf[e] : 0.f;
-#pragma unroll
-          for (int h = 0; h < GP; ++h)
-#pragma unroll
-            for (int e = 0; e < E; ++e) o[h][e] = fmaf(p[h], vf[e], o[h][e]);
-        }
+          for (int e = 0; e < E; ++e) o[h][e] *= c[h];
       }
+      const float p1 = ok ? __builtin_amdgcn_exp2f(s1 - m1) : 0.f;
+      z1 += p1;
+      float p[GP], vf[E];
+      row_all_gather<GP, LPR>(p1, p, cc);
+      unpack4(t.v[w], vf);
+#pragma unroll
+      for (int e = 0; e < E; ++e) vf[e] = ok ? vf[e] : 0.f;   // (what is read in its place may hold an infinity)
+#pragma unroll
+      for (int h = 0; h < GP; ++h)
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[h][e] = fmaf(p[h], vf[e], o[h][e]);
+    }
+  };
+  int u = u0 + wave, step = 0, part = 0;
+  if (u < u1) {
+    int pages = load_pages(a, table, u, u1, len), pages_behind = pages;
+    Part even, odd;
+    bool more = true;
+    load(even, pages, step, u, part);
+    auto turn = [&](const Part& now, Part& next) {
+      if (++part == kParts) {
+        part = 0;
+        u += kAttWaves;
+        ++step;
+        more = u < u1;
+        if ((step & 31) == 16) pages_behind = load_pages(a, table, u + 16 * kAttWaves, u1, len);
+        if ((step & 31) == 0) pages = pages_behind;
+      }
+      if (more) load(next, pages, step, u, part);
+      compute(now);
+    };
+    while (more) {
+      turn(even, odd);
+      if (!more) break;
+      turn(odd, even);
     }
   }
   // merge the lane groups of the wave, which saw different rows
@@ -443,15 +487,15 @@ __device__ __forceinline__ void attend_matrix(const PagedArgs& a, int r, int hea
   }
 }
 
-// grid: kAttGroups workgroups or fewer (a share of kMinUnits units for each of the most that there can be).
+// grid: groups_per_cu workgroups for every CU, or fewer (a share of kMinUnits units for each of the most that there can be).
 template <typename T, int D, int GP, bool FP8>
-__global__ void __launch_bounds__(kAttThreads, sizeof(T) == 4 && GP == 16 ? 2 : 3) paged_attention_kernel(PagedArgs a) {
+__global__ void __launch_bounds__(kAttThreads, (groups_per_cu(sizeof(T), D, GP))) paged_attention_kernel(PagedArgs a) {
   __shared__ float red_o[kAttWaves][GP][D];
   __shared__ float red_m[kAttWaves][GP], red_z[kAttWaves][GP];
   const int id = blockIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  auto units = [&](int r) { return (long long)((row_len(a, r) + kUnit - 1) / kUnit) * a.Hkv; };
+  auto units = [&](int r) { return (row_len(a, r) + kUnit - 1) / kUnit; };
   long long all = 0, shares = 0, beg = 0, end = 0;
-  const RowOfUnit at = locate_row(a.R, units, [&](long long total) {
+  const RowOfUnit at = locate_row(a.R, a.Hkv, units, [&](long long total) {
     all = total;
     shares = min((total + kMinUnits - 1) / kMinUnits, (long long)gridDim.x);
     if (id < shares) {
@@ -460,14 +504,9 @@ __global__ void __launch_bounds__(kAttThreads, sizeof(T) == 4 && GP == 16 ? 2 : 
     }
     return beg < end ? beg : -1ll;
   });
-  // rows without positions, dealt to all workgroups
-  for (int r = id; r < a.R; r += gridDim.x)
-    if (row_len(a, r) == 0)
-      for (int i = threadIdx.x; i < a.Hq * D; i += kAttThreads) store_elem(a.out + r * a.out_stride + (size_t)i * sizeof(T), 0.f, T{});
-
   int2 cut = make_int2(0, 0);
   if (at.row >= 0) {
-    int r = at.row, len = row_len(a, r), n = (len + kUnit - 1) / kUnit;
+    int r = at.row, len = row_len(a, r), n = at.size;
     int head = (int)((beg - at.first) / n), u = (int)((beg - at.first) - (long long)head * n);
     while (true) {
       const int take = (int)min((long long)(n - u), end - beg);
@@ -495,44 +534,63 @@ __global__ void __launch_bounds__(kAttThreads, sizeof(T) == 4 && GP == 16 ? 2 : 
     }
   }
   if (threadIdx.x == 0) a.cut[id] = cut;
+  // rows without positions, dealt to all workgroups
+  for (int r = id; r < a.R; r += gridDim.x)
+    if (row_len(a, r) == 0)
+      for (int i = threadIdx.x; i < a.Hq * D; i += kAttThreads) store_elem(a.out + r * a.out_stride + (size_t)i * sizeof(T), 0.f, T{});
 }
 
-// grid (workgroups of the first kernel, G), 256 threads = 256 / D lanes of shares x D columns: joins the pieces of the
-// (row, kv head) that share blockIdx.x cuts, one query head each.
+// grid (workgroups of the first kernel, G): joins the pieces of the (row, kv head) that share blockIdx.x cuts, one query
+// head each.  Four columns per thread, kJoinLanes pieces side by side and 16 of each on their way together: a request cut
+// into 128 pieces takes two rounds.  (One column per thread, two pieces side by side, eight on their way: 5 us for 512
+// shares of seven heads, 10 us for three long requests.)
+constexpr int kJoinLanes = 4;
 template <typename T, int D>
-__global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs a) {
-  constexpr int kLanes = 256 / D, U = 8;
-  __shared__ float lds_o[kLanes][D], lds_m[kLanes], lds_z[kLanes];
-  const int id = blockIdx.x, h = blockIdx.y, j = threadIdx.x % D, lane = threadIdx.x / D;
+__global__ void __launch_bounds__(kJoinLanes * D / 4) paged_join_kernel(PagedArgs a) {
+  constexpr int Q = D / 4, U = 16;
+  __shared__ float4 lds_o[kJoinLanes][Q];
+  __shared__ float lds_m[kJoinLanes], lds_z[kJoinLanes];
+  const int id = blockIdx.x, h = blockIdx.y, j = threadIdx.x % Q, lane = threadIdx.x / Q;
   const int2 cut = a.cut[id];
   if (cut.y == 0) return;
   const int n = cut.y + 1;   // pieces: slot 1 of share id, slot 0 of the shares behind it
-  float mn = kLeast, zs = 0.f, os = 0.f;
-  for (int s0 = lane; s0 < n; s0 += kLanes * U) {
-    float m[U], z[U], o[U];
+  float mn = kLeast, zs = 0.f;
+  float4 os = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [](float4& acc, const float4& x, float c) {
+    acc.x = fmaf(x.x, c, acc.x); acc.y = fmaf(x.y, c, acc.y); acc.z = fmaf(x.z, c, acc.z); acc.w = fmaf(x.w, c, acc.w);
+  };
+  auto round = [&](int s0, auto count) {
+    constexpr int N = decltype(count)::value;
+    float2 mz[N];
+    float4 o[N];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int s = min(s0 + u * kLanes, n - 1);
-      const float* p = a.part + ((size_t)(2 * (id + s) + (s == 0 ? 1 : 0)) * a.G + h) * (D + 2);
-      m[u] = p[D];
-      z[u] = p[D + 1];
-      o[u] = p[j];
+    for (int u = 0; u < N; ++u) {
+      const int s = min(s0 + u * kJoinLanes, n - 1);
+      const size_t at = (size_t)(2 * (id + s) + (s == 0 ? 1 : 0)) * a.G + h;
+      mz[u] = a.part_mz[at];
+      o[u] = *reinterpret_cast<const float4*>(a.part + at * D + 4 * j);
     }
+    // (all of them are asked for before any is used: under the conditions below each load would wait for itself)
+#pragma unroll
+    for (int u = 0; u < N; ++u) asm volatile("" : "+v"(o[u].x), "+v"(o[u].y), "+v"(o[u].z), "+v"(o[u].w), "+v"(mz[u].x), "+v"(mz[u].y));
     float top = mn;
 #pragma unroll
-    for (int u = 0; u < U; ++u) top = fmaxf(top, m[u]);   // (a piece that is repeated changes no maximum)
+    for (int u = 0; u < N; ++u) top = fmaxf(top, mz[u].x);   // (a piece that is repeated changes no maximum)
     const float c0 = __builtin_amdgcn_exp2f(mn - top);
     zs *= c0;
-    os *= c0;
+    os.x *= c0; os.y *= c0; os.z *= c0; os.w *= c0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool in = s0 + u * kLanes < n;
-      const float c = __builtin_amdgcn_exp2f(m[u] - top);
-      zs = in ? fmaf(z[u], c, zs) : zs;
-      os = in ? fmaf(o[u], c, os) : os;
+    for (int u = 0; u < N; ++u) {
+      const bool in = s0 + u * kJoinLanes < n;
+      const float c = in ? __builtin_amdgcn_exp2f(mz[u].x - top) : 0.f;
+      zs = fmaf(in ? mz[u].y : 0.f, c, zs);
+      add(os, make_float4(in ? o[u].x : 0.f, in ? o[u].y : 0.f, in ? o[u].z : 0.f, in ? o[u].w : 0.f), c);
     }
     mn = top;
-  }
+  };
+  int s0 = lane;
+  for (; s0 + U / 4 * kJoinLanes < n; s0 += U * kJoinLanes) round(s0, std::integral_constant<int, U>());
+  if (s0 < n) round(s0, std::integral_constant<int, U / 4>());
   lds_o[lane][j] = os;
   if (j == 0) {
     lds_m[lane] = mn;
@@ -542,21 +600,25 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs a) {
   if (lane != 0) return;
   mn = lds_m[0];
 #pragma unroll
-  for (int w = 1; w < kLanes; ++w) mn = fmaxf(mn, lds_m[w]);
-  zs = os = 0.f;
+  for (int w = 1; w < kJoinLanes; ++w) mn = fmaxf(mn, lds_m[w]);
+  zs = 0.f;
+  os = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-  for (int w = 0; w < kLanes; ++w) {
+  for (int w = 0; w < kJoinLanes; ++w) {
     const float c = __builtin_amdgcn_exp2f(lds_m[w] - mn);
     zs = fmaf(lds_z[w], c, zs);
-    os = fmaf(lds_o[w][j], c, os);
+    add(os, lds_o[w][j], c);
   }
   const int r = cut.x / a.Hkv, head = cut.x - r * a.Hkv;
-  store_elem(a.out + r * a.out_stride + ((size_t)(head * a.G + h) * D + j) * sizeof(T), zs == 0.f ? 0.f : os / zs, T{});
+  char* dst = a.out + r * a.out_stride + ((size_t)(head * a.G + h) * D + 4 * j) * sizeof(T);
+  const float x[4] = {os.x, os.y, os.z, os.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) store_elem(dst + i * sizeof(T), zs == 0.f ? 0.f : x[i] / zs, T{});
 }
 
 struct PagedPlan {
   int groups, GP;
-  size_t part_bytes, ws_bytes;
+  size_t part_bytes, mz_bytes, ws_bytes;
 };
 
 static meda_status make_paged_plan(const meda_page_pool* pool, const meda_paged_params* p, PagedPlan* pl) {
@@ -571,7 +633,7 @@ static meda_status make_paged_plan(const meda_page_pool* pool, const meda_paged_
   if (st != MEDA_OK) return st;
   const int G = p->n_q_heads / pool->n_kv_heads;
   const int64_t most = (int64_t)p->max_blocks * pool->page_size;
-  if (G > kMaxGroup || p->n_rows > 65536 || most > INT32_MAX || most * pool->n_kv_heads > (1ll << 34)) return MEDA_ERR_UNSUPPORTED;
+  if (G > kMaxGroup || p->n_rows > 65536 || most > (1 << 29) || most * pool->n_kv_heads > (1ll << 34)) return MEDA_ERR_UNSUPPORTED;
   if ((int64_t)p->n_rows * pool->n_kv_heads > INT32_MAX) return MEDA_ERR_UNSUPPORTED;
   const int elt = dtype_bytes(p->dtype);
   const int64_t row = (int64_t)p->n_q_heads * pool->head_dim, far = 1ll << 40;
@@ -580,11 +642,13 @@ static meda_status make_paged_plan(const meda_page_pool* pool, const meda_paged_
   if (p->q_stride * elt % 16 || p->out_stride * elt % 16) return MEDA_ERR_INVALID_ARG;
   if (p->q_stride > far || p->out_stride > far || p->table_stride > far || p->len_stride > far) return MEDA_ERR_UNSUPPORTED;
   const int64_t units = (most + kUnit - 1) / kUnit * pool->n_kv_heads;     // of one row, at most
-  const int64_t shares = units > kAttGroups * (int64_t)kMinUnits ? kAttGroups : (units * p->n_rows + kMinUnits - 1) / kMinUnits;
-  pl->groups = (int)(shares < kAttGroups ? shares : kAttGroups);
   pl->GP = G <= 1 ? 1 : (G <= 2 ? 2 : (G <= 4 ? 4 : (G <= 8 ? 8 : 16)));
-  pl->part_bytes = ((size_t)2 * pl->groups * G * (pool->head_dim + 2) * sizeof(float) + 255) / 256 * 256;
-  pl->ws_bytes = pl->part_bytes + ((size_t)pl->groups * sizeof(int2) + 255) / 256 * 256;
+  const int64_t most_groups = kCus * groups_per_cu(elt, pool->head_dim, pl->GP);
+  const int64_t shares = units > most_groups * kMinUnits ? most_groups : (units * p->n_rows + kMinUnits - 1) / kMinUnits;
+  pl->groups = (int)(shares < most_groups ? shares : most_groups);
+  pl->part_bytes = ((size_t)2 * pl->groups * G * pool->head_dim * sizeof(float) + 255) / 256 * 256;
+  pl->mz_bytes = ((size_t)2 * pl->groups * G * sizeof(float2) + 255) / 256 * 256;
+  pl->ws_bytes = pl->part_bytes + pl->mz_bytes + ((size_t)pl->groups * sizeof(int2) + 255) / 256 * 256;
   return MEDA_OK;
 }
 
@@ -593,7 +657,7 @@ static hipError_t launch_paged(const PagedPlan& pl, const PagedArgs& a, hipStrea
   hipLaunchKernelGGL((paged_attention_kernel<T, D, GP, FP8>), dim3(pl.groups), dim3(kAttThreads), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(pl.groups, a.G), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(pl.groups, a.G), dim3(kJoinLanes * D / 4), 0, s, a);
   return hipGetLastError();
 }
 template <typename T, int D, bool FP8>
@@ -635,7 +699,8 @@ meda_status meda_paged_attention(const meda_page_pool* pool, const meda_paged_pa
   a.out = static_cast<char*>(out);
   a.table = table; a.lens = lens;
   a.part = static_cast<float*>(workspace);
-  a.cut = reinterpret_cast<int2*>(static_cast<char*>(workspace) + pl.part_bytes);
+  a.part_mz = reinterpret_cast<float2*>(static_cast<char*>(workspace) + pl.part_bytes);
+  a.cut = reinterpret_cast<int2*>(static_cast<char*>(workspace) + pl.part_bytes + pl.mz_bytes);
   a.q_stride = (p.q_stride ? p.q_stride : row) * elt;
   a.out_stride = (p.out_stride ? p.out_stride : row) * elt;
   a.table_stride = p.table_stride ? p.table_stride : p.max_blocks;

@@ -41,9 +41,9 @@ __global__ void __launch_bounds__(kLocateThreads) paged_store_kernel(StoreArgs a
   constexpr int kOut = CODES ? 1 : (int)sizeof(T);
   const int lane = threadIdx.x & 63, sub = lane / LPR, cc = lane - sub * LPR;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  auto pieces = [&](int r) { return (long long)((stored_rows(a, r) + kPiece - 1) / kPiece) * a.pool.Hkv; };
+  auto pieces = [&](int r) { return (stored_rows(a, r) + kPiece - 1) / kPiece; };
   long long beg = 0, end = 0;
-  const RowOfUnit at = locate_row(a.R, pieces, [&](long long total) {
+  const RowOfUnit at = locate_row(a.R, a.pool.Hkv, pieces, [&](long long total) {
     beg = total * blockIdx.x / gridDim.x;
     end = total * (blockIdx.x + 1) / gridDim.x;
     return beg < end ? beg : -1ll;
@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(kLocateThreads) paged_store_kernel(StoreArgs a
   if (at.row < 0) return;
   int r = at.row;
   long long first = at.first;                 // number of row r's first piece
-  int rows = stored_rows(a, r), per_head = (rows + kPiece - 1) / kPiece;
+  int rows = stored_rows(a, r), per_head = at.size;
   for (long long u = beg + wave; u < end; u += kLocateThreads / 64) {
     while (u >= first + (long long)per_head * a.pool.Hkv) {   // (u < end: there is such a row)
       first += (long long)per_head * a.pool.Hkv;
@@ -127,7 +127,7 @@ meda_status meda_paged_store(const meda_page_pool* pool, const meda_store_params
   if (p.n_src_rows < 0 || p.table_stride < 0 || p.len_stride < 0 || p.n_seqs < 1 || p.n_layers < 1 || p.max_blocks < 1) return MEDA_ERR_INVALID_ARG;
   st = check_types(p.dtype, pool->dtype);
   if (st != MEDA_OK) return st;
-  if ((int64_t)p.n_seqs * p.n_layers > 65536 || (int64_t)p.max_blocks * pool->page_size > INT32_MAX) return MEDA_ERR_UNSUPPORTED;
+  if ((int64_t)p.n_seqs * p.n_layers > 65536 || (int64_t)p.max_blocks * pool->page_size > (1 << 29)) return MEDA_ERR_UNSUPPORTED;
   if ((int64_t)p.max_blocks * pool->page_size * pool->n_kv_heads > (1ll << 34) || p.n_src_rows > (1ll << 40)) return MEDA_ERR_UNSUPPORTED;
   if (p.table_stride && p.table_stride < p.max_blocks) return MEDA_ERR_INVALID_ARG;
   if (!k_rows || !v_rows || !layer_len || !layer_off || !lens || !table) return MEDA_ERR_INVALID_ARG;

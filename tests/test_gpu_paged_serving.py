@@ -163,6 +163,7 @@ def test_graph_replays_and_streams():
     stream.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(stream):
         body(other, o_out)
+    torch.cuda.synchronize()                        # (what follows changes x on the first stream)
     for i in range(40):                             # across several page boundaries
         pos.fill_(i)
         for t in x:
