@@ -541,13 +541,14 @@ __global__ void __launch_bounds__(kAttThreads, (groups_per_cu(sizeof(T), D, GP))
 }
 
 // grid (workgroups of the first kernel, G): joins the pieces of the (row, kv head) that share blockIdx.x cuts, one query
-// head each.  Four columns per thread, kJoinLanes pieces side by side and 16 of each on their way together: a request cut
-// into 128 pieces takes two rounds.  (One column per thread, two pieces side by side, eight on their way: 5 us for 512
-// shares of seven heads, 10 us for three long requests.)
-constexpr int kJoinLanes = 4;
+// head each.  Four columns per thread, kJoinLanes pieces side by side and eight of each on their way together: a request cut
+// into 128 pieces takes two rounds.  768 shares of seven heads, most of them cut in two or three: 4.3 us; three long fp32
+// requests cut into 128 pieces per head: 6.7 us (half as many pieces side by side 5.5 and 9.5; one column per thread, two
+// pieces side by side 5 and 10).
+constexpr int kJoinLanes = 8;
 template <typename T, int D>
 __global__ void __launch_bounds__(kJoinLanes * D / 4) paged_join_kernel(PagedArgs a) {
-  constexpr int Q = D / 4, U = 16;
+  constexpr int Q = D / 4, U = 8;
   __shared__ float4 lds_o[kJoinLanes][Q];
   __shared__ float lds_m[kJoinLanes], lds_z[kJoinLanes];
   const int id = blockIdx.x, h = blockIdx.y, j = threadIdx.x % Q, lane = threadIdx.x / Q;

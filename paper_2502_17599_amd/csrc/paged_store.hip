@@ -27,6 +27,12 @@ struct StoreArgs {
 
 constexpr int kPiece = 16;      // rows
 
+__device__ __forceinline__ void store8_stream(void* p, const uint2& v) {  // see store16_stream
+  typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
+  const u32x2_t t = {v.x, v.y};
+  __builtin_nontemporal_store(t, reinterpret_cast<u32x2_t*>(p));
+}
+
 // rows of row r that are stored, per kv head
 __device__ __forceinline__ int stored_rows(const StoreArgs& a, int r) {
   const int most = a.max_blocks << a.pool.page_log2;
@@ -85,14 +91,14 @@ __global__ void __launch_bounds__(kLocateThreads) paged_store_kernel(StoreArgs a
       for (int w = 0; w < U; ++w) {
         const int i = w * RPW + sub;
         if constexpr (!CODES) {
-          if (i < n) *reinterpret_cast<uint4*>(dst + (size_t)i * (D * kOut) + cc * 16) = x[kv][w];
+          if (i < n) store16_stream(dst + (size_t)i * (D * kOut) + cc * 16, x[kv][w]);
         } else {
           float f[E];
           uint32_t c[E / 4];
           RP::unpack(x[kv][w], f);
           const float scale = quantize_row<E, LPR>(f, c);
           if (i < n) {
-            if constexpr (E == 8) *reinterpret_cast<uint2*>(dst + (size_t)i * D + cc * 8) = make_uint2(c[0], c[1]);
+            if constexpr (E == 8) store8_stream(dst + (size_t)i * D + cc * 8, make_uint2(c[0], c[1]));
             else *reinterpret_cast<uint32_t*>(dst + (size_t)i * D + cc * 4) = c[0];
             if (cc == 0) (kv ? a.pool.vs : a.pool.ks)[scale0 + i] = scale;
           }
@@ -106,7 +112,7 @@ template <typename T, int D, bool CODES>
 static hipError_t launch_store(const StoreArgs& a, hipStream_t s) {
   // a wave for every 8 pieces that all source rows would make, up to 8 workgroups per CU
   long long groups = (a.n_src_rows / kPiece + 31) / 32 + 1;
-  if (groups > 256 * 8) groups = 256 * 8;
+  if (groups > 256 * 16) groups = 256 * 16;
   hipLaunchKernelGGL((paged_store_kernel<T, D, CODES>), dim3((unsigned)groups), dim3(kLocateThreads), 0, s, a);
   return hipGetLastError();
 }

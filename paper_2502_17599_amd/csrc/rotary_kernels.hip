@@ -1,8 +1,9 @@
 // Rotary positions of queries and keys, and the step that writes new tokens into the pages of a cache.
 //
 // Both stream rows once: a row is held by LPR = row bytes / 16 lanes, which exchange the halves of the pairs among
-// themselves, so that an output may be its own input.  The angles depend on the token alone: a wave takes 64 / LPR tokens,
-// computes the sines once and walks over heads with them in registers.
+// themselves, so that an output may be its own input.  The angles depend on the token alone: a workgroup takes
+// 4 * 64 / LPR tokens, its threads compute the sines of their pairs once, into LDS, and every wave walks over heads with the
+// factors of its tokens in registers, kAhead rows per lane on their way together.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -33,20 +34,47 @@ struct RotaryArgs {
 
 enum RotaryTo { kToRows, kToPages, kToCodes };   // k: strided rows, pages of the same type, 8-bit pages (k and v)
 
+constexpr int kAhead = 4;
+
 // grid (token groups, parts of the heads), 256 threads: 4 * 64 / LPR tokens, heads_per_part of the Hq + Hk (+ Hkv) heads.
-template <typename T, int D, RotaryTo TO>
+// STREAM: rows are written past the caches.
+template <typename T, int D, RotaryTo TO, bool STREAM>
 __global__ void __launch_bounds__(256) rotary_kernel(RotaryArgs a) {
   using RP = RowPiece<T>;
   constexpr int E = RP::kElems, LPR = D / E, TPW = 64 / LPR;
-  __shared__ float exchange[4][TPW][D];
+  __shared__ float exchange[4][TPW][D];            // first the pairs of the workgroup's tokens, as float2 [4 * TPW][D / 2]
+  float2* pairs = reinterpret_cast<float2*>(&exchange[0][0][0]);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane / LPR, cc = lane - sub * LPR;
-  const long long token = (long long)blockIdx.x * (4 * TPW) + wave * TPW + sub;
+  const long long token0 = (long long)blockIdx.x * (4 * TPW), token = token0 + wave * TPW + sub;
   const bool live = token < a.tokens;
   const long long t = live ? token : a.tokens - 1;   // lanes past the end repeat the last token and store nothing
 
-  float c[E], s[E];
+  const int nq = a.q.heads, nk = a.k.heads, nv = TO == kToRows ? 0 : a.pool.Hkv;
+  const int h0 = blockIdx.y * a.heads_per_part, h1 = min(h0 + a.heads_per_part, nq + nk + nv);
+  auto fetch = [&](uint4 (&raw)[kAhead], int h) {
 #pragma unroll
-  for (int i = 0; i < E; ++i) rotary_factors(a.plan, t, cc * E + i, c[i], s[i]);
+    for (int u = 0; u < kAhead; ++u) {
+      const int x = min(h + u, h1 - 1);
+      const char* src = x < nq ? a.q.in + t * a.q.in_token + x * a.q.in_head
+                               : (x < nq + nk ? a.k.in + t * a.k.in_token + (x - nq) * a.k.in_head
+                                              : a.v + t * a.v_token + (x - nq - nk) * a.v_head);
+      raw[u] = load16_stream(src + cc * 16);
+    }
+  };
+  uint4 raw[kAhead];
+  fetch(raw, h0);
+
+  float c[E], s[E];
+  if (a.plan.half > 0) {
+    for (int i = threadIdx.x; i < 4 * TPW * a.plan.half; i += 256) {
+      const int x = i / a.plan.half, pair = i - x * a.plan.half;
+      pairs[x * (D / 2) + pair] = rotary_pair(a.plan, min(token0 + x, a.tokens - 1), pair);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < E; ++i) rotary_factors(a.plan, pairs + (wave * TPW + sub) * (D / 2), cc * E + i, c[i], s[i]);
+    __syncthreads();   // the exchange below uses the same memory
+  }
 
   // where the token's rows go in the pages
   size_t place = 0, scale_place = 0;
@@ -62,33 +90,31 @@ __global__ void __launch_bounds__(256) rotary_kernel(RotaryArgs a) {
     }
   }
 
-  const int nq = a.q.heads, nk = a.k.heads, nv = TO == kToRows ? 0 : a.pool.Hkv;
-  const int h0 = blockIdx.y * a.heads_per_part, h1 = min(h0 + a.heads_per_part, nq + nk + nv);
-  for (int h = h0; h < h1; ++h) {
+  auto finish = [&](const uint4& x, int h) {
     const bool is_q = h < nq, is_v = h >= nq + nk;
     const int g = is_q ? h : (is_v ? h - nq - nk : h - nq);
-    const char* src = is_q ? a.q.in + t * a.q.in_token + g * a.q.in_head
-                           : (is_v ? a.v + t * a.v_token + g * a.v_head : a.k.in + t * a.k.in_token + g * a.k.in_head);
+    const bool turned = !is_v && a.plan.half > 0;
     float f[E];
-    const uint4 raw = *reinterpret_cast<const uint4*>(src + cc * 16);
-    RP::unpack(raw, f);
-    if (!is_v && a.plan.half > 0) {
-      float o[E];
-      rotary_partners<E, LPR>(a.plan, cc, f, o, exchange[wave][sub]);
-#pragma unroll
-      for (int i = 0; i < E; ++i)   // (elements past rot_dim stay as they are: infinity * 0 would not)
-        f[i] = cc * E + i < 2 * a.plan.half ? fmaf(f[i], c[i], o[i] * s[i]) : f[i];
+    uint4 y = x;
+    if (turned) {
+      rotary_turn<T, LPR>(a.plan, cc, x, c, s, f, exchange[wave][sub]);
+      if (TO != kToCodes || is_q) y = pack_row(f);
     }
     if (TO == kToRows || is_q) {
       const Rows& to = is_q ? a.q : a.k;
-      if (live) *reinterpret_cast<uint4*>(to.out + t * to.out_token + g * to.out_head + cc * 16) = RP::pack(f);
+      char* dst = to.out + t * to.out_token + g * to.out_head + cc * 16;
+      if (live) {
+        if constexpr (STREAM) store16_stream(dst, y);
+        else *reinterpret_cast<uint4*>(dst) = y;
+      }
     } else {
       char* pages = is_v ? a.pool.v : a.pool.k;
       const size_t row = place + ((size_t)g << a.pool.page_log2) * (D * kOut);
       if constexpr (TO == kToPages) {
-        if (slot_ok) *reinterpret_cast<uint4*>(pages + row + cc * 16) = RP::pack(f);
+        if (slot_ok) *reinterpret_cast<uint4*>(pages + row + cc * 16) = y;
       } else {
         uint32_t w[E / 4];
+        if (!turned) RP::unpack(x, f);
         const float scale = quantize_row<E, LPR>(f, w);
         if (slot_ok) {
           if constexpr (E == 8) *reinterpret_cast<uint2*>(pages + row + cc * 8) = make_uint2(w[0], w[1]);
@@ -97,6 +123,15 @@ __global__ void __launch_bounds__(256) rotary_kernel(RotaryArgs a) {
         }
       }
     }
+  };
+  for (int h = h0; h < h1; h += kAhead) {
+    uint4 now[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) now[u] = raw[u];
+    if (h + kAhead < h1) fetch(raw, h + kAhead);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (h + u < h1) finish(now[u], h + u);
   }
 }
 
@@ -105,12 +140,26 @@ static hipError_t launch_rotary(RotaryArgs a, hipStream_t s) {
   constexpr int TPB = 4 * 64 / (D / RowPiece<T>::kElems);
   const int heads = a.q.heads + a.k.heads + (TO == kToRows ? 0 : a.pool.Hkv);
   const long long groups = (a.tokens + TPB - 1) / TPB;
-  // few tokens: the heads are dealt to more workgroups
-  long long parts = (2048 + groups - 1) / groups;
+  // The heads are dealt to several workgroups where there are few, but every part computes the sines of its tokens again: parts
+  // of 12 heads or more, and of fewer only where CUs would have nothing to do.  (4001 tokens, 48 heads to 8 bits: 36, 29, 27 us
+  // with parts of 3, 6 and 12 heads; 4095 tokens, 40 fp32 heads: 34, 31, 32 with 5, 10 and 20; 37376 tokens, 32 heads: 123 and
+  // 128 with 16 and 32.)
+  const long long many = (4096 + groups - 1) / groups, some = (heads + 11) / 12, least = (512 + groups - 1) / groups;
+  long long parts = some > least ? some : least;
+  if (parts > many) parts = many;
   if (parts > heads) parts = heads;
   a.heads_per_part = (int)((heads + parts - 1) / parts);
   const unsigned n_parts = (unsigned)((heads + a.heads_per_part - 1) / a.heads_per_part);
-  hipLaunchKernelGGL((rotary_kernel<T, D, TO>), dim3((unsigned)groups, n_parts), dim3(256), 0, s, a);
+  const dim3 grid((unsigned)groups, n_parts), block(256);
+  // Rows that do not fit the 256 MB of the last-level cache are gone before anybody reads them there (306 MB: 123 us with
+  // ordinary stores, 119 past the caches; 84 MB: 31 and 32).
+  if constexpr (TO == kToRows) {
+    if (a.tokens * heads * D * (long long)sizeof(T) >= (256ll << 20)) {
+      hipLaunchKernelGGL((rotary_kernel<T, D, TO, true>), grid, block, 0, s, a);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((rotary_kernel<T, D, TO, false>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 
