@@ -291,7 +291,7 @@ typedef struct {
  */
 typedef struct {
   int64_t n_pages;     /* 1 .. 2^31 - 1                                                                 */
-  int32_t n_rows;      /* R, 1 .. 65536; R * max_blocks < 2^31                                          */
+  int32_t n_rows;      /* R, 1 .. 65536; R * max_blocks <= 2^30                                         */
   int32_t max_blocks;  /* columns of the table, >= 1; max_blocks * page_size < 2^31                     */
   int32_t page_size;   /* 16, 32, 64, 128 or 256                                                        */
   int32_t max_new;     /* columns of slots, >= 0                                                        */

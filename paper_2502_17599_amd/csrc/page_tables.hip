@@ -30,6 +30,7 @@ struct PageUpdate {
 };
 
 constexpr int kPlanThreads = 1024;
+constexpr int kAloneSlots = 8192;   // slots that one workgroup writes on its own
 
 struct RowNeed {
   int len, held, want;   // length, pages held, new positions asked for (negative: ended)
@@ -81,20 +82,31 @@ __device__ __forceinline__ void write_slot(const PageUpdate& a, int r, int pop, 
   a.slots[(size_t)r * a.max_new + i] = slot;
 }
 
-// One workgroup: the scan over the rows.  plan[r], the new lengths, what was granted, the ring's new state.
-__global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(PageUpdate a) {
+// What a row's place in the scan says: pages needed by the rows before it, pages given back before it, its length, the new
+// positions it is granted (-1: ended).
+struct RowPlan {
+  int base, behind, len, count;
+};
+struct PlanTotals {
+  int head, free;    // of the ring before the call
+  int taken, given;  // pages
+};
+
+// The scan over the rows by one workgroup of kPlanThreads threads: keep(r, plan) for every row, in the thread that has it.
+// (Sums stay below R * max_blocks <= 2^30.)  Everything of lens and the ring's state has been read when it returns.
+template <typename Keep>
+__device__ __forceinline__ PlanTotals plan_rows(const PageUpdate& a, Keep keep) {
   __shared__ int wave_need[kPlanThreads / 64], wave_give[kPlanThreads / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int head, free;
-  ring_state(a, head, free);
-  int need_before = 0, give_before = 0;   // of the rows before this round's (sums stay below R * max_blocks < 2^31)
-  int taken = 0;                          // pages granted up to here by this thread's rows
+  PlanTotals t{0, 0, 0, 0};
+  ring_state(a, t.head, t.free);
+  int need_before = 0, give_before = 0, taken = 0;
   for (int base = 0; base < a.R; base += kPlanThreads) {
     const int r = base + tid;
     RowNeed n{0, 0, 0, 0, 0, false};
     if (r < a.R) n = row_need(a, r);
     const int need_in = wave_inclusive_sum(n.need), give_in = wave_inclusive_sum(n.give);
-    __syncthreads();
+    if (base > 0) __syncthreads();
     if (lane == 63) {
       wave_need[wave] = need_in;
       wave_give[wave] = give_in;
@@ -109,29 +121,81 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(PageUpdate a) {
       give_before += wave_give[w];
     }
     if (r < a.R) {
-      const bool grant = n.fits && (n.need == 0 || need_to <= free);
-      const int count = n.want < 0 ? -1 : (grant ? n.want : 0);
-      taken += grant ? n.need : 0;
-      a.plan[r] = make_int4(ring_at(a, head, grant ? need_to - n.need : 0), ring_at(a, head, (long long)free + (give_to - n.give)),
-                            n.len, count);
-      a.lens_out[r] = n.want < 0 ? 0 : n.len + count;
-      if (a.granted) a.granted[r] = count;
+      const bool grant = n.fits && (n.need == 0 || need_to <= t.free);
+      if (grant && n.need > 0) taken = need_to;   // (granted needs are a prefix of the sum)
+      keep(r, RowPlan{need_to - n.need, give_to - n.give, n.len, n.want < 0 ? -1 : (grant ? n.want : 0)});
     }
   }
-  taken = wave_sum(taken);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) taken = max(taken, __shfl_xor(taken, o, kWave));
   __syncthreads();
   if (lane == 0) wave_need[wave] = taken;
   __syncthreads();
-  if (tid == 0) {
-    long long all = 0;
-    for (int w = 0; w < kPlanThreads / 64; ++w) all += wave_need[w];
-    const long long left = free - all + give_before;
-    a.state_out[0] = ring_at(a, head, all);
-    a.state_out[1] = left > a.n_pages ? a.n_pages : left;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 64; ++w) t.taken = max(t.taken, wave_need[w]);
+  t.given = give_before;
+  return t;
+}
+
+__device__ __forceinline__ void write_row(const PageUpdate& a, int r, const RowPlan& p) {
+  a.lens_out[r] = p.count < 0 ? 0 : p.len + p.count;
+  if (a.granted) a.granted[r] = p.count;
+}
+__device__ __forceinline__ void write_state(const PageUpdate& a, const PlanTotals& t) {
+  const long long left = (long long)t.free - t.taken + t.given;
+  a.state_out[0] = ring_at(a, t.head, t.taken);
+  a.state_out[1] = left > a.n_pages ? a.n_pages : left;
+}
+
+// Everything in one launch, up to kFusedRows rows: the scan, and then every entry on its own, whatever row it belongs to
+// (the row of the n-th page taken or given back is searched in the scan's sums).  grid: one workgroup, or, where lens_out and
+// state_out are arrays of their own, any number: every workgroup scans all rows and takes a part of the entries.
+constexpr int kFusedRows = 2048;
+__global__ void __launch_bounds__(kPlanThreads) page_update_kernel(PageUpdate a) {
+  __shared__ RowPlan rows[kFusedRows];
+  const PlanTotals t = plan_rows(a, [&](int r, const RowPlan& p) {
+    rows[r] = p;
+    if (blockIdx.x == 0) write_row(a, r, p);
+  });
+  if (blockIdx.x == 0 && threadIdx.x == 0) write_state(a, t);
+  const int at = blockIdx.x * kPlanThreads + threadIdx.x, step = gridDim.x * kPlanThreads, page = 1 << a.page_log2;
+  // the last row whose sum is not above n
+  auto row_of = [&](int n, int RowPlan::*sum) {
+    int lo = 0, hi = a.R;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (rows[mid].*sum <= n) lo = mid; else hi = mid;
+    }
+    return lo;
+  };
+  for (int n = at; n < t.taken; n += step) {
+    const int r = row_of(n, &RowPlan::base), held = (rows[r].len + page - 1) >> a.page_log2;
+    a.table[(size_t)r * a.max_blocks + held + (n - rows[r].base)] = a.ring[ring_at(a, t.head, n)];
+  }
+  for (int n = at; n < t.given; n += step) {
+    const int r = row_of(n, &RowPlan::behind);
+    a.ring[ring_at(a, t.head, (long long)t.free + n)] = a.table[(size_t)r * a.max_blocks + (n - rows[r].behind)];
+  }
+  const unsigned entries = (unsigned)a.R * (unsigned)a.max_new;
+  for (unsigned n = at; n < entries; n += step) {
+    const int r = (int)(n / (unsigned)a.max_new), i = (int)(n - (unsigned)r * (unsigned)a.max_new);
+    const RowPlan p = rows[r];
+    write_slot(a, r, ring_at(a, t.head, p.count > 0 ? p.base : 0), (p.len + page - 1) >> a.page_log2, p.len, p.count, i);
   }
 }
 
-// grid (R, parts): the entries of one row.
+// More rows, or many slots beside lengths that are updated in place: the scan by itself, plan[r] for every row ...
+__global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(PageUpdate a) {
+  int head, free;
+  ring_state(a, head, free);
+  const PlanTotals t = plan_rows(a, [&](int r, const RowPlan& p) {
+    a.plan[r] = make_int4(ring_at(a, head, p.count > 0 ? p.base : 0), ring_at(a, head, (long long)free + p.behind), p.len, p.count);
+    write_row(a, r, p);
+  });
+  if (threadIdx.x == 0) write_state(a, t);
+}
+
+// ... and the entries of one row.  grid (R, parts).
 __global__ void __launch_bounds__(256) page_fill_kernel(PageUpdate a) {
   const int r = blockIdx.x, at = blockIdx.y * 256 + threadIdx.x, step = gridDim.y * 256;
   const int4 plan = a.plan[r];
@@ -147,6 +211,14 @@ __global__ void __launch_bounds__(256) page_fill_kernel(PageUpdate a) {
 }
 
 static hipError_t launch_page_update(const PageUpdate& a, hipStream_t s) {
+  const long long entries = (long long)a.R * a.max_new;
+  const bool in_place = a.lens_out == a.lens || a.state_out == a.state;
+  if (a.R <= kFusedRows && (entries <= kAloneSlots || (!in_place && entries < (1ll << 31)))) {
+    long long groups = entries <= kAloneSlots ? 1 : (entries + 4 * kPlanThreads - 1) / (4 * kPlanThreads);
+    if (groups > 256) groups = 256;
+    hipLaunchKernelGGL(page_update_kernel, dim3((unsigned)groups), dim3(kPlanThreads), 0, s, a);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL(page_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -174,7 +246,7 @@ meda_status meda_page_update(const meda_page_params* params, const int32_t* lens
   const meda_page_params& p = *params;
   if (p.n_pages < 1 || p.n_rows < 1 || p.max_blocks < 1 || p.max_new < 0) return MEDA_ERR_INVALID_ARG;
   if (p.n_pages > INT32_MAX || p.n_rows > 65536 || !valid_page_size(p.page_size)) return MEDA_ERR_UNSUPPORTED;
-  if ((int64_t)p.n_rows * p.max_blocks > INT32_MAX || (int64_t)p.max_blocks * p.page_size > INT32_MAX) return MEDA_ERR_UNSUPPORTED;
+  if ((int64_t)p.n_rows * p.max_blocks > (1 << 30) || (int64_t)p.max_blocks * p.page_size > INT32_MAX) return MEDA_ERR_UNSUPPORTED;
   if (!lens || !n_new || !table || !free_ring || !free_state || !lens_out || !free_state_out) return MEDA_ERR_INVALID_ARG;
   if (p.max_new > 0 && !slots) return MEDA_ERR_INVALID_ARG;
   const uintptr_t words = (uintptr_t)lens | (uintptr_t)n_new | (uintptr_t)table | (uintptr_t)free_ring | (uintptr_t)lens_out | (uintptr_t)granted;
