@@ -369,7 +369,7 @@ typedef struct {
   int64_t len_stride;      /* 0 = 1                                                                     */
   int32_t n_seqs;          /* N >= 1                                                                    */
   int32_t n_layers;        /* L >= 1; N * L <= 65536                                                    */
-  int32_t max_blocks;      /* >= 1; max_blocks * page_size <= 2^29, times Hkv <= 2^34                   */
+  int32_t max_blocks;      /* >= 1; max_blocks * page_size <= 2^29, times Hkv and rows <= 2^34          */
   int32_t dtype;           /* type of k_rows and v_rows                                                 */
 } meda_store_params;
 meda_status meda_paged_store(const meda_page_pool* pool, const meda_store_params* params, const void* k_rows,
@@ -391,7 +391,7 @@ typedef struct {
   int64_t q_stride, out_stride, table_stride, len_stride;
   int32_t n_rows;          /* R, 1 .. 65536                                                             */
   int32_t n_q_heads;       /* Hq, Hq % Hkv == 0, Hq / Hkv <= 16                                         */
-  int32_t max_blocks;      /* >= 1; max_blocks * page_size <= 2^29, times Hkv <= 2^34                   */
+  int32_t max_blocks;      /* >= 1; max_blocks * page_size <= 2^29, times Hkv and rows <= 2^34          */
   int32_t dtype;
   float softmax_scale;     /* 0 -> 1/sqrt(head_dim)                                                     */
 } meda_paged_params;

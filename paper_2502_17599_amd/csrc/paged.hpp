@@ -68,81 +68,107 @@ static inline meda_status check_types(int dtype, int pool_dtype) {
 
 constexpr int kLocateThreads = 256;
 
-// A number that is the same in every lane, as a value the compiler knows to be uniform.
-__device__ __forceinline__ long long uniform(long long v) {
-  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)v), hi = __builtin_amdgcn_readfirstlane((unsigned)(v >> 32));
-  return (long long)(((unsigned long long)hi << 32) | lo);
+// `total` units in `shares` contiguous shares of total / shares or one more: the first unit of share `id`, and the share of a
+// unit.  (Numbers of units are 32-bit: the host refuses sizes that could have 2^31 of them.)
+struct Shares {
+  unsigned each, more;   // units of a share; the number of shares, the first ones, that have one more
+  __device__ __forceinline__ Shares(unsigned total, unsigned shares) {
+    each = total / shares;
+    more = total - each * shares;
+  }
+  __device__ __forceinline__ unsigned first(unsigned id) const { return each * id + min(id, more); }
+  __device__ __forceinline__ unsigned share_of(unsigned unit) const {   // (each >= 1)
+    const unsigned border = (each + 1) * more;
+    const bool low = unit < border;
+    return (low ? unit : unit - border) / (low ? each + 1 : each) + (low ? 0u : more);
+  }
+};
+// Rows of at most `positions` positions in units of `unit` of them: whether all units together have 32-bit numbers.
+static inline bool few_units(int64_t rows, int64_t positions, int64_t heads, int64_t unit) {
+  const int64_t each = (positions + unit - 1) / unit * heads;
+  return each <= INT32_MAX && rows * each <= INT32_MAX;
 }
 
 struct RowOfUnit {
   int row;          // -1: no unit at all
   int size;         // units of the row, per head
-  long long first;  // number of the row's first unit
+  unsigned first;   // number of the row's first unit
 };
 
-// Rows 0 .. R-1 of units(r) >= 0 units in each of Hkv heads, numbered row after row and head after head: finds the row of
-// unit number pick(total), as the same value in every thread of a workgroup of kLocateThreads.  pick sees the total and must
-// give a number below it, or a negative one for nothing.
+// Rows 0 .. R-1 of units(r) >= 0 units in each of Hkv heads, numbered row after row and head after head: finds for every
+// wave of a workgroup of kLocateThreads the row of unit number pick(wave), as the same value in all its lanes.  begin(total)
+// is called once before; a number that is no unit's is that of nothing.
 //
 // Up to 64 rows: every wave searches on its own, a lane per row (all workgroups of a launch begin with this, and the data's
 // latency is all it should cost).  More: every thread adds up the same number of consecutive rows, with two barriers.
-template <typename Units, typename Pick>
-__device__ __forceinline__ RowOfUnit locate_row(int R, int Hkv, Units units, Pick pick) {
-  const int lane = threadIdx.x & 63;
+template <typename Units, typename Begin, typename Pick>
+__device__ __forceinline__ RowOfUnit locate_row(int R, unsigned Hkv, Units units, Begin begin, Pick pick) {
+  constexpr int kWaves = kLocateThreads / 64;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (R <= 64) {
-    const int mine = lane < R ? units(lane) : 0;
-    // (64 rows of at most 2^25 units each: the sum fits 32 bits)
-    const unsigned end = (unsigned)wave_inclusive_sum(mine);
-    const long long total = (long long)(unsigned)__builtin_amdgcn_readlane((int)end, 63) * Hkv;
-    const long long unit = pick(total);
+    const unsigned mine = lane < R ? (unsigned)units(lane) : 0u;
+    const unsigned end = (unsigned)wave_inclusive_sum((int)mine);
+    begin((unsigned)__builtin_amdgcn_readlane((int)end, 63) * Hkv);
+    const unsigned unit = pick(wave);
+    const unsigned long long b = __ballot(unit >= (end - mine) * Hkv && unit < end * Hkv);
     RowOfUnit out{-1, 0, 0};
-    const unsigned long long b = __ballot(unit >= (long long)(end - (unsigned)mine) * Hkv && unit < (long long)end * Hkv);
-    if (unit >= 0 && b != 0ull) {
+    if (b != 0ull) {
       out.row = __ffsll(b) - 1;
-      out.size = __builtin_amdgcn_readlane(mine, out.row);
-      out.first = (long long)(unsigned)__builtin_amdgcn_readlane((int)(end - (unsigned)mine), out.row) * Hkv;
+      out.size = __builtin_amdgcn_readlane((int)mine, out.row);
+      out.first = (unsigned)__builtin_amdgcn_readlane((int)(end - mine), out.row) * Hkv;
     }
     return out;
   }
-  __shared__ long long sums[kLocateThreads / 64];
-  __shared__ RowOfUnit found;
-  const int wave = threadIdx.x >> 6;
+  __shared__ unsigned sums[kWaves];
+  __shared__ RowOfUnit found[kWaves];
+  constexpr int kKept = 8;   // rows of a thread that are kept in registers: loaded together, and once
   const int per = (R + kLocateThreads - 1) / kLocateThreads;
   const int r0 = min((int)threadIdx.x * per, R), r1 = min(r0 + per, R);
-  long long mine = 0;
-  for (int r = r0; r < r1; ++r) mine += units(r);
-  long long end = mine;
+  unsigned mine = 0;
+  int kept[kKept];
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const long long up = __shfl_up(end, o, kWave);
-    if (lane >= o) end += up;
+  for (int i = 0; i < kKept; ++i) {
+    kept[i] = r0 + i < r1 ? units(r0 + i) : 0;
+    mine += (unsigned)kept[i];
   }
+#pragma unroll 4
+  for (int r = r0 + kKept; r < r1; ++r) mine += (unsigned)units(r);
+  unsigned end = (unsigned)wave_inclusive_sum((int)mine);
   if (lane == 63) sums[wave] = end;
-  if (threadIdx.x == 0) found = RowOfUnit{-1, 0, 0};
+  if (threadIdx.x < kWaves) found[threadIdx.x] = RowOfUnit{-1, 0, 0};
   __syncthreads();
-  long long total = 0;
+  unsigned total = 0;
 #pragma unroll
-  for (int w = 0; w < kLocateThreads / 64; ++w) {
+  for (int w = 0; w < kWaves; ++w) {
     end += w < wave ? sums[w] : 0;
     total += sums[w];
   }
-  const long long unit = pick(uniform(total) * Hkv);
-  if (unit >= (end - mine) * Hkv && unit < end * Hkv) {
-    long long at = end - mine;
-    for (int r = r0; r < r1; ++r) {
-      const int n = units(r);
-      if (unit < (at + n) * Hkv) {
-        found = RowOfUnit{r, n, at * Hkv};
-        break;
+  begin((unsigned)__builtin_amdgcn_readfirstlane((int)total) * Hkv);
+#pragma unroll 1
+  for (int w = 0; w < kWaves; ++w) {
+    const unsigned unit = pick(w);
+    if (unit >= (end - mine) * Hkv && unit < end * Hkv) {
+      unsigned at = end - mine;
+      RowOfUnit hit{-1, 0, 0};
+#pragma unroll
+      for (int i = 0; i < kKept; ++i) {
+        if (hit.row < 0 && unit < (at + kept[i]) * Hkv) hit = RowOfUnit{r0 + i, kept[i], at * Hkv};
+        at += kept[i];
       }
-      at += n;
+#pragma unroll 1
+      for (int r = r0 + kKept; r < r1 && hit.row < 0; ++r) {
+        const int n = units(r);
+        if (unit < (at + n) * Hkv) hit = RowOfUnit{r, n, at * Hkv};
+        at += n;
+      }
+      found[w] = hit;
     }
   }
   __syncthreads();
   RowOfUnit out;
-  out.row = __builtin_amdgcn_readfirstlane(found.row);
-  out.size = __builtin_amdgcn_readfirstlane(found.size);
-  out.first = uniform(found.first);
+  out.row = __builtin_amdgcn_readfirstlane(found[wave].row);
+  out.size = __builtin_amdgcn_readfirstlane(found[wave].size);
+  out.first = (unsigned)__builtin_amdgcn_readfirstlane((int)found[wave].first);
   return out;
 }
 

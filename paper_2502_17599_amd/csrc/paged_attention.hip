@@ -19,18 +19,11 @@
 namespace meda {
 
 constexpr int kAttThreads = kLocateThreads, kAttWaves = kAttThreads / 64;
-constexpr int kUnit = 32;         // positions: a step of one wave
+constexpr int kBlock = 16;        // positions of one matrix instruction; they lie in one page
 constexpr int kMinUnits = 4;      // a workgroup's share, at least: a step per wave
 constexpr int kMaxGroup = 16;     // query heads per kv head
-// Workgroups per CU, and waves per SIMD, as many as the registers allow.  All workgroups of a launch are at work at once,
-// each on one share, and every CU has equally many of them: 512 workgroups of which three fit a CU were spread unevenly
-// (64 requests, 435 MB: 95 us against 86 with 768), and with two or three rounds of shorter shares the workgroups' searches
-// and the joins cost more than the evener end gained (104 and 111 us against 99, before the pages of 32 steps were loaded
-// at once).
-constexpr int groups_per_cu(int q_bytes, int d, int gp) {
-  return q_bytes == 4 ? (gp <= 2 ? 4 : (gp <= 8 ? 3 : 2)) : (d == 64 ? 4 : 3);
-}
-constexpr int kCus = 256;
+// positions of a unit, a step of one wave: two blocks, of 4-byte rows one (as many bytes)
+constexpr int unit_positions(int bytes) { return bytes == 4 ? kBlock : 2 * kBlock; }
 
 struct PagedArgs {
   Pool pool;
@@ -52,30 +45,39 @@ __device__ __forceinline__ int row_len(const PagedArgs& a, int r) {
   return min(max(a.lens[r * a.len_stride], 0), a.max_blocks << a.pool.page_log2);
 }
 
-// The pages of the units u, u + kAttWaves, .. of a wave (32 of them, two blocks of 16 positions each): lane 2 i + b holds
-// that of block b of the i-th.  One load for 32 steps: a load of its own in every step would have to be waited for, and with
-// it, as loads come back in order, for all rows that are on their way (64 requests, 435 MB: 95 us against 81).
+// A maximum starts at the least finite number, not at -infinity: every finite logit replaces or equals it, a logit of
+// -infinity has the weight exp2(-inf) = 0 under it, and differences of maxima are never inf - inf.
+constexpr float kLeast = -__FLT_MAX__;
+
+// The pages of the 64 / BLOCKS units from u on: lane BLOCKS i + b holds that of block b of the i-th.  One load for many
+// steps: a load of its own in every step would have to be waited for, and with it, as loads come back in order, for all
+// rows that are on their way.
+template <int BLOCKS>
 __device__ __forceinline__ int load_pages(const PagedArgs& a, const int32_t* table, int u, int u1, int len) {
   const int lane = threadIdx.x & 63;
-  const int pos = min(u + kAttWaves * (lane >> 1), u1 - 1) * kUnit;     // (units past the share repeat its last one)
-  const int p = pos + 16 * (lane & 1);
+  const int pos = min(u + lane / BLOCKS, u1 - 1) * (BLOCKS * kBlock);   // (units past the last one repeat it)
+  const int p = pos + kBlock * (lane % BLOCKS);
   return table[(p < len ? p : pos) >> a.pool.page_log2];                // a block behind the end repeats the first one
 }
 
-// Where a unit's two blocks of 16 positions lie, as byte offsets of (page, head, place) and scale indexes.
+// Where a unit's blocks lie, as byte offsets of (page, head, place) and scale indexes.
+template <int BLOCKS>
 struct UnitPages {
-  size_t at[2];
-  size_t scale[2];
-  bool ok[2];      // the page exists
+  size_t at[BLOCKS];
+  size_t scale[BLOCKS];
+  bool ok[BLOCKS];      // the page exists
+  bool full;            // all positions count
 };
-template <int ROW_BYTES>
-__device__ __forceinline__ UnitPages unit_pages(const PagedArgs& a, int pages, int step, int head, int pos, int len) {
-  UnitPages u;
+template <int ROW_BYTES, int BLOCKS>
+__device__ __forceinline__ UnitPages<BLOCKS> unit_pages(const PagedArgs& a, int pages, int step, int head, int pos, int len) {
+  UnitPages<BLOCKS> u;
+  u.full = pos + BLOCKS * kBlock <= len;
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const int p = pos + 16 * b, q = p < len ? p : pos;
-    const int page = __builtin_amdgcn_readlane(pages, 2 * (step & 31) + b);
+  for (int b = 0; b < BLOCKS; ++b) {
+    const int p = pos + kBlock * b, q = p < len ? p : pos;
+    const int page = __builtin_amdgcn_readlane(pages, (BLOCKS * step + b) & 63);
     u.ok[b] = page >= 0 && page < a.pool.n_pages;
+    u.full = u.full && u.ok[b];
     const size_t safe = u.ok[b] ? page : 0;
     const size_t place = ((size_t)head << a.pool.page_log2) + (q & ((1 << a.pool.page_log2) - 1));
     u.at[b] = safe * a.pool.page_bytes + place * ROW_BYTES;
@@ -84,98 +86,138 @@ __device__ __forceinline__ UnitPages unit_pages(const PagedArgs& a, int pages, i
   return u;
 }
 
-// A maximum starts at the least finite number, not at -infinity: every finite logit replaces or equals it, a logit of
-// -infinity has the weight exp2(-inf) = 0 under it, and differences of maxima are never inf - inf.
-constexpr float kLeast = -__FLT_MAX__;
-
-// ---- bf16 and 8-bit pages: both products on the matrix unit ---------------------------------------------------------
+// ---- both products on the matrix unit -------------------------------------------------------------------------------
 //
-// Lane (c, g) = (l % 16, l / 16).  logits D[key][col] = sum_d K[key][d] Q[col][d]: the lane holds 8 elements of key c per
-// k-step and block of 16 keys, and receives the logits of head c % GP for the keys 4 g + i of every block.  The second
-// product O[row][col] += sum_key P[row][key] V[key][col] contracts over the keys in the order (lane group, register), so
-// its weights are what the lane has; its values are the same 8 keys at d / 16 columns, transposed in registers.
-// A weight enters as the sum of two bf16 numbers, rows c / GP = 0 and 1 of the product (what the first leaves is exact and
-// not zero, and 2^-16 of the weight is lost at most: a 128th of the output's own rounding), so that groups of up to 8
-// heads need one instruction per 16 columns; groups of 9 to 16 take two, one per part.  8-bit rows: codes become bf16
-// exactly, the key's scale multiplies the logit and the value's scale the weight.
-template <int D>
-struct AttState {
-  float m, z;           // of head c % GP; m is the same in the four lane groups
-  f32x4_t acc[D / 16];  // acc[j][r]: output column (d/16) c + j, product row 4 g + r
-};
+// Lane (c, g) = (l % 16, l / 16).  logits D[key][col] = sum_d K[key][d] Q[col][d], blocks of 16 keys: the lane holds elements
+// of key c, the same ones of query head c % GP, and receives the logits of that head for the keys 4 g + i of every block.
+// The second product O[row][col] += sum_key P[row][key] V[key][col] contracts over the keys in an order in which its
+// weights are what the lane has.
+//   bf16 and 8 bits (16x16x32): a weight enters as the sum of two bf16 numbers, rows c / GP = 0 and 1 of the product (what the
+// first leaves is exact and not zero, and 2^-16 of the weight is lost at most: a 128th of the output's own rounding), so that
+// groups of up to 8 heads need one instruction per 16 columns; groups of 9 to 16 take two, one per part.  The values are 8
+// keys at d / 16 columns, transposed in registers.  8-bit rows: codes become bf16 exactly, the key's scale multiplies the
+// logit and the value's scale the weight.
+//   fp32 (16x16x4): products and sums in fp32.  Four instructions use up the 16 bytes that a lane loads of a key or of a value;
+// the values' column is 4 c + e of 64.  (On the vector unit, with the dot products summed over lanes, groups of 8 and
+// 16 heads were bound by its instructions: 3.9 and 2.0 TB/s.)
+template <typename T, int D, int GP, bool FP8>
+struct Attend {
+  static constexpr bool F32 = sizeof(T) == 4;
+  static constexpr int kEl = F32 ? 4 : (FP8 ? 1 : 2), kRowBytes = D * kEl;
+  static constexpr int BLOCKS = unit_positions(sizeof(T)) / kBlock, kUnit = BLOCKS * kBlock, kKeys = 4 * BLOCKS;
+  static constexpr int KL = kRowBytes / 64;          // 16-byte loads per key and lane
+  static constexpr int VW = D / 16 * kEl / 4;        // dwords of a value piece
+  static constexpr int PE = D / 16;                  // 16-column accumulators
+  static constexpr int QV = F32 ? D / 16 : D / 32;   // 16-byte pieces of a query
 
-template <int D, int GP, bool FP8>
-__device__ __forceinline__ void attend_units(AttState<D>& st, const uint4 (&qp)[D / 32], const PagedArgs& a,
-                                             const int32_t* table, int head, int u0, int u1, int len) {
-  constexpr int KS = D / 32, PE = D / 16, kEl = FP8 ? 1 : 2, kRowBytes = D * kEl;
-  constexpr int KL = D * kEl / 64;            // 16-byte loads per key and lane
-  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int part = (c / GP) & 1;
   struct Unit {
-    uint32_t k[2][KL][4], v[8][PE * kEl / 4];
+    uint4 k[BLOCKS][KL];
+    uint32_t v[kKeys][VW];
     float scale;
   };
+  float m, z;           // of head c % GP; m is the same in the four lane groups
+  f32x4_t acc[PE];      // acc[j][r]: output column column(j), product row 4 g + r
+  uint4 q[QV];
+
+  static __device__ __forceinline__ int column(int c, int j) { return F32 ? 64 * (j / 4) + 4 * c + j % 4 : PE * c + j; }
+
+  __device__ __forceinline__ void begin(const PagedArgs& a, int r, int head) {
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    m = kLeast;
+    z = 0.f;
+#pragma unroll
+    for (int j = 0; j < PE; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    const char* src = a.q + r * a.q_stride + (size_t)(head * a.G + c % GP) * (D * sizeof(T));
+#pragma unroll
+    for (int k = 0; k < QV; ++k) {
+      // the elements that the key's loads bring (16 bytes of codes are two steps of the product)
+      const int e0 = F32 ? 16 * k + 4 * g : (FP8 ? 64 * (k / 2) + 16 * g + 8 * (k & 1) : 32 * k + 8 * g);
+      q[k] = make_uint4(0u, 0u, 0u, 0u);
+      if (c % GP < a.G) q[k] = *reinterpret_cast<const uint4*>(src + e0 * sizeof(T));
+    }
+  }
+
   // MASKED: some of the unit's positions lie behind the end or in a page that does not exist.  Positions behind the end
   // repeat the last one (their weights are zero).
-  auto load_keys = [&](Unit& t, const UnitPages& up, int pos, auto masked) {
-    constexpr bool MASKED = decltype(masked)::value;
+  template <bool MASKED>
+  __device__ __forceinline__ static void load_keys(const PagedArgs& a, Unit& t, const UnitPages<BLOCKS>& up, int pos, int len) {
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int last = min(len - 1 - pos - 16 * b, 15), top = last < 0 ? min(len - 1 - pos, 15) : last;
+    for (int b = 0; b < BLOCKS; ++b) {
+      const int last = min(len - 1 - pos - kBlock * b, 15), top = last < 0 ? min(len - 1 - pos, 15) : last;
       const char* src = a.pool.k + up.at[b] + (unsigned)((MASKED ? min(c, top) : c) * kRowBytes + 16 * g);
 #pragma unroll
-      for (int k = 0; k < KL; ++k) {
-        const uint4 x = load16_stream(src + 64 * k);
-        t.k[b][k][0] = x.x; t.k[b][k][1] = x.y; t.k[b][k][2] = x.z; t.k[b][k][3] = x.w;
-      }
+      for (int k = 0; k < KL; ++k) t.k[b][k] = load16_stream(src + 64 * k);
     }
-  };
-  auto load_values = [&](Unit& t, const UnitPages& up, int pos, auto masked) {
-    constexpr bool MASKED = decltype(masked)::value;
+  }
+  template <bool MASKED>
+  __device__ __forceinline__ static void load_values(const PagedArgs& a, Unit& t, const UnitPages<BLOCKS>& up, int pos, int len) {
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int last = min(len - 1 - pos - 16 * b, 15), top = last < 0 ? min(len - 1 - pos, 15) : last;
+    for (int b = 0; b < BLOCKS; ++b) {
+      const int last = min(len - 1 - pos - kBlock * b, 15), top = last < 0 ? min(len - 1 - pos, 15) : last;
       const char* src = a.pool.v + up.at[b];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        load_piece<PE * kEl>(src + (unsigned)((MASKED ? min(4 * g + i, top) : 4 * g + i) * kRowBytes + c * PE * kEl), t.v[4 * b + i]);
+      for (int i = 0; i < 4; ++i) {
+        const char* row = src + (unsigned)((MASKED ? min(4 * g + i, top) : 4 * g + i) * kRowBytes);
+        if constexpr (F32) {
+#pragma unroll
+          for (int x = 0; x < VW / 4; ++x) {
+            const uint4 y = load16_stream(row + 256 * x + 16 * c);
+            uint32_t* to = &t.v[4 * b + i][4 * x];
+            to[0] = y.x; to[1] = y.y; to[2] = y.z; to[3] = y.w;
+          }
+        } else {
+          load_piece<VW * 4>(row + c * (VW * 4), t.v[4 * b + i]);
+        }
+      }
       // the scales of the 8 keys that this row of 16 lanes has logits for: lanes 0..7 the keys', 8..15 the values'
       if constexpr (FP8) {
         const int row = 4 * g + (c & 3);
         if (((c >> 2) & 1) == b) t.scale = (c < 8 ? a.pool.ks : a.pool.vs)[up.scale[b] + (MASKED ? min(row, top) : row)];
       }
     }
-  };
-  auto logits = [&](const Unit& rows, float (&t)[8]) {
+  }
+
+  __device__ __forceinline__ void logits(const Unit& rows, float (&t)[kKeys]) const {
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < BLOCKS; ++b) {
       f32x4_t s4 = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        uint4 kp;
-        if constexpr (FP8) kp = e4m3x8_to_bf16x8(make_uint2(rows.k[b][k / 2][2 * (k & 1)], rows.k[b][k / 2][2 * (k & 1) + 1]));
-        else kp = make_uint4(rows.k[b][k][0], rows.k[b][k][1], rows.k[b][k][2], rows.k[b][k][3]);
-        s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kp), __builtin_bit_cast(bf16x8_t, qp[k]), s4, 0, 0, 0);
+      for (int k = 0; k < QV; ++k) {
+        if constexpr (F32) {
+          const uint4 x = rows.k[b][k], y = q[k];
+          s4 = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.x), __uint_as_float(y.x), s4, 0, 0, 0);
+          s4 = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.y), __uint_as_float(y.y), s4, 0, 0, 0);
+          s4 = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.z), __uint_as_float(y.z), s4, 0, 0, 0);
+          s4 = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.w), __uint_as_float(y.w), s4, 0, 0, 0);
+        } else {
+          uint4 x;
+          if constexpr (FP8) x = e4m3x8_to_bf16x8((k & 1) ? make_uint2(rows.k[b][k / 2].z, rows.k[b][k / 2].w) : make_uint2(rows.k[b][k / 2].x, rows.k[b][k / 2].y));
+          else x = rows.k[b][k];
+          s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, q[k]), s4, 0, 0, 0);
+        }
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) t[4 * b + i] = s4[i];
     }
-  };
-  auto finish = [&](Unit& rows, const UnitPages& up, int pos, float (&t)[8], auto masked) {
-    constexpr bool MASKED = decltype(masked)::value;
+  }
+
+  template <bool MASKED>
+  __device__ __forceinline__ void finish(const PagedArgs& a, Unit& rows, const UnitPages<BLOCKS>& up, int pos, int len, float (&t)[kKeys]) {
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, part = (c / GP) & 1;
     float sk[8], sv[8];
-    bool in[8];
+    bool in[kKeys];
     if constexpr (FP8) {
       row_broadcast<0>(rows.scale * a.scale_log2, sk);
       row_broadcast<8>(rows.scale, sv);
     }
     float bm = kLeast;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < kKeys; ++e) {
       t[e] *= FP8 ? sk[e] : a.scale_log2;
       if constexpr (MASKED) {
-        in[e] = up.ok[e >> 2] && pos + 16 * (e >> 2) + 4 * g + (e & 3) < len;
+        in[e] = up.ok[e >> 2] && pos + kBlock * (e >> 2) + 4 * g + (e & 3) < len;
         t[e] = in[e] ? t[e] : -INFINITY;
 #pragma unroll
         for (uint32_t& x : rows.v[e]) x = in[e] ? x : 0u;   // what is read in its place may hold an infinity
@@ -183,355 +225,298 @@ __device__ __forceinline__ void attend_units(AttState<D>& st, const uint4 (&qp)[
       bm = fmaxf(bm, t[e]);
     }
     bm = group_max(bm);
-    if (__ballot(bm > st.m) != 0ull) {  // a new maximum of some head: rescale what that head has so far (rare)
-      const float mn = fmaxf(st.m, bm);
-      const float c1 = __builtin_amdgcn_exp2f(st.m - mn);
-      st.z *= c1;
-      st.m = mn;
+    if (__ballot(bm > m) != 0ull) {  // a new maximum of some head: rescale what that head has so far (rare)
+      const float mn = fmaxf(m, bm);
+      const float c1 = __builtin_amdgcn_exp2f(m - mn);
+      z *= c1;
+      m = mn;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const float cr = __shfl(c1, 4 * g + r, kWave);  // product row 4 g + r belongs to the head of lane column 4 g + r
 #pragma unroll
-        for (int j = 0; j < PE; ++j) st.acc[j][r] *= cr;
+        for (int j = 0; j < PE; ++j) acc[j][r] *= cr;
       }
     }
-    uint32_t pa[4], pb[4];
+    float w[kKeys];
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      uint32_t x[2], y[2];
+    for (int e = 0; e < kKeys; ++e) {
+      float p = __builtin_amdgcn_exp2f(t[e] - m);
+      w[e] = FP8 ? fmaf(p, sv[e], 0.f) : p;  // the sum takes the sign of a zero
+      if constexpr (MASKED) {
+        p = in[e] ? p : 0.f;
+        w[e] = in[e] ? w[e] : 0.f;
+      }
+      z += p;
+    }
+    if constexpr (F32) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float p = __builtin_amdgcn_exp2f(t[e + u] - st.m);
-        float w = FP8 ? fmaf(p, sv[e + u], 0.f) : p;  // the sum takes the sign of a zero
-        if constexpr (MASKED) {
-          p = in[e + u] ? p : 0.f;
-          w = in[e + u] ? w : 0.f;
+      for (int e = 0; e < kKeys; ++e)
+#pragma unroll
+        for (int j = 0; j < PE; ++j)
+          acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[e], __uint_as_float(rows.v[e][j]), acc[j], 0, 0, 0);
+    } else {
+      uint32_t pa[4], pb[4];
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        uint32_t x[2], y[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const float hi = weight_part(w[e + u]), lo = w[e + u] - hi;
+          x[u] = __float_as_uint(GP == 16 || part == 0 ? hi : lo);
+          y[u] = __float_as_uint(lo);
         }
-        st.z += p;
-        const float hi = weight_part(w), lo = w - hi;
-        x[u] = __float_as_uint(GP == 16 || part == 0 ? hi : lo);
-        y[u] = __float_as_uint(lo);
+        pa[e / 2] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302u);
+        pb[e / 2] = __builtin_amdgcn_perm(y[1], y[0], 0x07060302u);
       }
-      pa[e / 2] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302u);
-      pb[e / 2] = __builtin_amdgcn_perm(y[1], y[0], 0x07060302u);
-    }
-    const bf16x8_t wa = __builtin_bit_cast(bf16x8_t, make_uint4(pa[0], pa[1], pa[2], pa[3]));
-    const bf16x8_t wb = __builtin_bit_cast(bf16x8_t, make_uint4(pb[0], pb[1], pb[2], pb[3]));
+      const bf16x8_t wa = __builtin_bit_cast(bf16x8_t, make_uint4(pa[0], pa[1], pa[2], pa[3]));
+      const bf16x8_t wb = __builtin_bit_cast(bf16x8_t, make_uint4(pb[0], pb[1], pb[2], pb[3]));
 #pragma unroll
-    for (int j2 = 0; j2 < PE / 2; ++j2) {  // two columns at a time: one dword of every row
-      uint32_t d[8];
+      for (int j2 = 0; j2 < PE / 2; ++j2) {  // two columns at a time: one dword of every row
+        uint32_t d[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if constexpr (FP8) d[e] = e4m3x2_to_bf16x2(rows.v[e][j2 / 2], (j2 & 1) != 0);
-        else d[e] = rows.v[e][j2];
+        for (int e = 0; e < 8; ++e) {
+          if constexpr (FP8) d[e] = e4m3x2_to_bf16x2(rows.v[e][j2 / 2], (j2 & 1) != 0);
+          else d[e] = rows.v[e][j2];
+        }
+        uint32_t lo[4], hi[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          lo[u] = __builtin_amdgcn_perm(d[2 * u + 1], d[2 * u], 0x05040100u);
+          hi[u] = __builtin_amdgcn_perm(d[2 * u + 1], d[2 * u], 0x07060302u);
+        }
+        const bf16x8_t v0 = __builtin_bit_cast(bf16x8_t, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+        const bf16x8_t v1 = __builtin_bit_cast(bf16x8_t, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+        acc[2 * j2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa, v0, acc[2 * j2], 0, 0, 0);
+        acc[2 * j2 + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa, v1, acc[2 * j2 + 1], 0, 0, 0);
+        if constexpr (GP == 16) {
+          acc[2 * j2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, v0, acc[2 * j2], 0, 0, 0);
+          acc[2 * j2 + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, v1, acc[2 * j2 + 1], 0, 0, 0);
+        }
       }
-      uint32_t lo[4], hi[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        lo[u] = __builtin_amdgcn_perm(d[2 * u + 1], d[2 * u], 0x05040100u);
-        hi[u] = __builtin_amdgcn_perm(d[2 * u + 1], d[2 * u], 0x07060302u);
-      }
-      const bf16x8_t v0 = __builtin_bit_cast(bf16x8_t, make_uint4(lo[0], lo[1], lo[2], lo[3]));
-      const bf16x8_t v1 = __builtin_bit_cast(bf16x8_t, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-      st.acc[2 * j2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa, v0, st.acc[2 * j2], 0, 0, 0);
-      st.acc[2 * j2 + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa, v1, st.acc[2 * j2 + 1], 0, 0, 0);
-      if constexpr (GP == 16) {
-        st.acc[2 * j2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, v0, st.acc[2 * j2], 0, 0, 0);
-        st.acc[2 * j2 + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, v1, st.acc[2 * j2 + 1], 0, 0, 0);
-      }
-    }
-  };
-
-  int u = u0 + wave, step = 0;
-  if (u >= u1) return;
-  auto full = [&](const UnitPages& up, int pos) { return pos + kUnit <= len && up.ok[0] && up.ok[1]; };
-  int pages = load_pages(a, table, u, u1, len), pages_behind = pages;
-  UnitPages up = unit_pages<kRowBytes>(a, pages, step, head, u * kUnit, len);
-  bool fast = full(up, u * kUnit);
-  Unit rows;
-  float t[8];
-  if (fast) load_keys(rows, up, 0, std::false_type());
-  while (fast) {
-    load_values(rows, up, 0, std::false_type());
-    const UnitPages cur = up;
-    u += kAttWaves;
-    ++step;
-    fast = u < u1;
-    if ((step & 31) == 16) pages_behind = load_pages(a, table, u + 16 * kAttWaves, u1, len);
-    if ((step & 31) == 0) pages = pages_behind;
-    if (fast) {
-      up = unit_pages<kRowBytes>(a, pages, step, head, u * kUnit, len);
-      fast = full(up, u * kUnit);
-    }
-    logits(rows, t);
-    if (fast) load_keys(rows, up, 0, std::false_type());  // in flight while this unit is finished
-    finish(rows, cur, 0, t, std::false_type());
-  }
-  for (; u < u1; u += kAttWaves) {   // the last unit of a row; units behind a missing page
-    up = unit_pages<kRowBytes>(a, load_pages(a, table, u, u1, len), 0, head, u * kUnit, len);
-    load_keys(rows, up, u * kUnit, std::true_type());
-    logits(rows, t);
-    load_values(rows, up, u * kUnit, std::true_type());
-    finish(rows, up, u * kUnit, t, std::true_type());
-  }
-}
-
-// ---- what a workgroup's waves have, merged: a finished output or a partial ------------------------------------------
-
-template <typename T, int H, int D>
-__device__ __forceinline__ void write_piece(const PagedArgs& a, bool whole, int slot, int r, int head,
-                                            const float (&red_o)[kAttWaves][H][D], const float (&red_m)[kAttWaves][H],
-                                            const float (&red_z)[kAttWaves][H]) {
-  for (int i = threadIdx.x; i < a.G * D; i += kAttThreads) {
-    const int h = i / D, j = i - h * D;
-    float mn = red_m[0][h];
-#pragma unroll
-    for (int w = 1; w < kAttWaves; ++w) mn = fmaxf(mn, red_m[w][h]);
-    float zs = 0.f, os = 0.f;
-#pragma unroll
-    for (int w = 0; w < kAttWaves; ++w) {
-      const float c = __builtin_amdgcn_exp2f(red_m[w][h] - mn);
-      zs = fmaf(red_z[w][h], c, zs);
-      os = fmaf(red_o[w][h][j], c, os);
-    }
-    if (whole) {
-      // (no weight at all, as where every page is missing: zeros)
-      store_elem(a.out + r * a.out_stride + ((size_t)(head * a.G + h) * D + j) * sizeof(T), zs == 0.f ? 0.f : os / zs, T{});
-    } else {
-      const size_t at = (size_t)slot * a.G + h;
-      a.part[at * D + j] = os;
-      if (j == 0) a.part_mz[at] = make_float2(mn, zs);
     }
   }
-}
 
-// ---- fp32 pages: the vector unit ------------------------------------------------------------------------------------
+  // Units [u0, u1) of a (row, kv head) with `len` positions.
+  __device__ __forceinline__ void units(const PagedArgs& a, const int32_t* table, int head, int u0, int u1, int len) {
+    constexpr int kAhead = 64 / BLOCKS;   // units whose pages one load brings
+    int pages = load_pages<BLOCKS>(a, table, u0, u1, len), pages_behind = pages, step = 0, u = u0;
+    UnitPages<BLOCKS> up = unit_pages<kRowBytes, BLOCKS>(a, pages, 0, head, u * kUnit, len);
+    Unit rows;
+    float t[kKeys];
+    bool fast = up.full;
+    if (fast) load_keys<false>(a, rows, up, 0, 0);
+    while (fast) {
+      load_values<false>(a, rows, up, 0, 0);
+      const UnitPages<BLOCKS> cur = up;
+      ++u;
+      ++step;
+      fast = u < u1;
+      if (step % kAhead == kAhead / 2) pages_behind = load_pages<BLOCKS>(a, table, u + kAhead / 2, u1, len);
+      if (step % kAhead == 0) pages = pages_behind;
+      if (fast) {
+        up = unit_pages<kRowBytes, BLOCKS>(a, pages, step, head, u * kUnit, len);
+        fast = up.full;
+      }
+      logits(rows, t);
+      if (fast) load_keys<false>(a, rows, up, 0, 0);  // in flight while this unit is finished
+      finish<false>(a, rows, cur, 0, 0, t);
+    }
+    for (; u < u1; ++u) {   // the last unit of a row; units behind a missing page
+      const int pos = u * kUnit;
+      up = unit_pages<kRowBytes, BLOCKS>(a, load_pages<BLOCKS>(a, table, u, u1, len), 0, head, pos, len);
+      load_keys<true>(a, rows, up, pos, len);
+      load_values<true>(a, rows, up, pos, len);
+      logits(rows, t);
+      finish<true>(a, rows, up, pos, len, t);
+    }
+  }
+
+  // The wave's sums of a piece: o[h][column], maximum and normaliser of the GP heads.  Product row 4 g + r is part
+  // (4 g + r) / GP of head (4 g + r) % GP: the two parts are summed (fp32: one part, the rows past it repeat it).
+  __device__ __forceinline__ void put(float (&o)[GP][D], float (&om)[GP], float (&oz)[GP]) const {
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    const float zs = group_sum(z);  // the four lane groups saw different keys of the same head
+    if (lane < GP) {
+      om[lane] = m;
+      oz[lane] = zs;
+    }
+#pragma unroll
+    for (int j = 0; j < PE; ++j) {
+      float* dst = &o[0][column(c, j)];
+      if constexpr (GP == 16 || F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (4 * g + i < GP) dst[(4 * g + i) * D] = acc[j][i];
+      } else if constexpr (GP == 8) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[j][i]), __float_as_uint(acc[j][i]), false, false);
+          if (g < 2) dst[(4 * g + i) * D] = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+        }
+      } else if constexpr (GP == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[j][i]), __float_as_uint(acc[j][i]), false, false);
+          if (g == 0) dst[i * D] = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < GP; ++i)
+          if (g == 0) dst[i * D] = acc[j][i] + acc[j][GP + i];
+      }
+    }
+  }
+};
+
+// ---- shares ---------------------------------------------------------------------------------------------------------
 //
-// A row is read by LPR = row bytes / 16 lanes, a wave takes 64 / LPR rows per step; every lane group keeps, per query head,
-// the running maximum, the normaliser and its piece of the weighted value sum over the rows it has seen.
-template <int D, int GP>
-__device__ __forceinline__ void attend_f32(const PagedArgs& a, int r, int head, const int32_t* table, int u0, int u1, int len,
-                                           float (&red_o)[GP][D], float (&red_m)[GP], float (&red_z)[GP]) {
-  // U steps' rows are on their way while U others are worked on (fewer where the heads need the registers)
-  constexpr int LPR = D / 4, MS = 64 / LPR, E = 4, U = GP <= 4 ? 4 : 2, kRowBytes = D * 4;
-  constexpr int kRows = U * MS, kParts = kUnit / kRows;   // positions of one part of a unit; a part lies in one block
-  static_assert(kRows <= 16, "a part lies in one page");
-  const int lane = threadIdx.x & 63, sub = lane / LPR, cc = lane - sub * LPR;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  uint4 qp[GP];
-#pragma unroll
-  for (int h = 0; h < GP; ++h)
-    qp[h] = *reinterpret_cast<const uint4*>(a.q + r * a.q_stride + (size_t)(head * a.G + (h < a.G ? h : 0)) * kRowBytes + cc * 16);
-  // running maximum and normaliser of the ONE head this lane evaluates (row_head), weighted value sums of all
-  float m1 = kLeast, z1 = 0.f, o[GP][E];
-#pragma unroll
-  for (int h = 0; h < GP; ++h)
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[h][e] = 0.f;
+// The units of all (row, kv head) pairs are numbered one pair after the other.  A workgroup takes a contiguous share of
+// them, each of its waves a contiguous quarter of the share: a wave that comes to the end of a pair goes on with the next
+// by itself, without a barrier (where pairs are a few units long, waves that worked on one pair together spent most of
+// their time on its beginning and its end: 256 requests of 40 to 600 positions, 222 MB, 68 us, 2000 rows of 10 to 300, 96 MB,
+// 53 us).  A pair that lies in one wave's quarter is written out by it.  The others leave pieces in LDS: a wave has at most
+// one that goes on from the wave before (slot 0) and one that begins in it and goes on (slot 1).  After one barrier the
+// workgroup adds up the pieces of every pair, and writes it out, or, where the pair goes on in other shares, as a piece of
+// the share: slot 0 and 1 again, in memory, for the join.
+struct WavePiece {
+  int pair;     // row * Hkv + head
+  int shares;   // slot 1: shares behind this one that the pair reaches into
+  bool there;
+  bool ends;    // slot 0: the pair ends in this wave
+};
 
-  struct Part {
-    uint4 k[U], v[U];
-    int n;           // its positions: fewer than kRows at the end, none in a page that does not exist
-  };
-  auto load = [&](Part& t, int pages, int step, int u, int part) {
-    const int pos = u * kUnit + part * kRows;
-    const int page = __builtin_amdgcn_readlane(pages, 2 * (step & 31) + part * kRows / 16);
-    const bool ok = page >= 0 && page < a.pool.n_pages;
-    t.n = ok ? min(max(len - pos, 0), kRows) : 0;
-    const size_t place = ((size_t)head << a.pool.page_log2) + (pos & ((1 << a.pool.page_log2) - 1));
-    const size_t at = (size_t)(ok ? page : 0) * a.pool.page_bytes + place * kRowBytes;
-#pragma unroll
-    for (int w = 0; w < U; ++w) {
-      const unsigned ro = (unsigned)(min(w * MS + sub, max(t.n - 1, 0)) * kRowBytes + cc * 16);
-      t.k[w] = load16_stream(a.pool.k + at + ro);
-      t.v[w] = load16_stream(a.pool.v + at + ro);
-    }
-  };
-  auto compute = [&](const Part& t) {
-#pragma unroll
-    for (int w = 0; w < U; ++w) {
-      const bool ok = w * MS + sub < t.n;
-      float s[GP];
-#pragma unroll
-      for (int h = 0; h < GP; ++h) s[h] = dot4(qp[h], t.k[w]);
-      row_reduce_scatter<GP, LPR>(s, cc);
-      const float s1 = ok ? s[0] * a.scale_log2 : -INFINITY;
-      if (__ballot(s1 > m1) != 0ull) {  // a new maximum of some head in some lane group (rare after the first rows)
-        const float mn = fmaxf(m1, s1);
-        const float c1 = __builtin_amdgcn_exp2f(m1 - mn);
-        z1 *= c1;
-        m1 = mn;
-        float c[GP];
-        row_all_gather<GP, LPR>(c1, c, cc);
-#pragma unroll
-        for (int h = 0; h < GP; ++h)
-#pragma unroll
-          for (int e = 0; e < E; ++e) o[h][e] *= c[h];
-      }
-      const float p1 = ok ? __builtin_amdgcn_exp2f(s1 - m1) : 0.f;
-      z1 += p1;
-      float p[GP], vf[E];
-      row_all_gather<GP, LPR>(p1, p, cc);
-      unpack4(t.v[w], vf);
-#pragma unroll
-      for (int e = 0; e < E; ++e) vf[e] = ok ? vf[e] : 0.f;   // (what is read in its place may hold an infinity)
-#pragma unroll
-      for (int h = 0; h < GP; ++h)
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[h][e] = fmaf(p[h], vf[e], o[h][e]);
-    }
-  };
-  int u = u0 + wave, step = 0, part = 0;
-  if (u < u1) {
-    int pages = load_pages(a, table, u, u1, len), pages_behind = pages;
-    Part even, odd;
-    bool more = true;
-    load(even, pages, step, u, part);
-    auto turn = [&](const Part& now, Part& next) {
-      if (++part == kParts) {
-        part = 0;
-        u += kAttWaves;
-        ++step;
-        more = u < u1;
-        if ((step & 31) == 16) pages_behind = load_pages(a, table, u + 16 * kAttWaves, u1, len);
-        if ((step & 31) == 0) pages = pages_behind;
-      }
-      if (more) load(next, pages, step, u, part);
-      compute(now);
-    };
-    while (more) {
-      turn(even, odd);
-      if (!more) break;
-      turn(odd, even);
-    }
-  }
-  // merge the lane groups of the wave, which saw different rows
-  float m[GP], z[GP];
-  row_all_gather<GP, LPR>(m1, m, cc);
-  row_all_gather<GP, LPR>(z1, z, cc);
-#pragma unroll
-  for (int x = LPR; x < 64; x <<= 1) {
-#pragma unroll
-    for (int h = 0; h < GP; ++h) {
-      const float mo = __shfl_xor(m[h], x, kWave), zo = __shfl_xor(z[h], x, kWave);
-      const float mn = fmaxf(m[h], mo);
-      const float c0 = __builtin_amdgcn_exp2f(m[h] - mn), c1 = __builtin_amdgcn_exp2f(mo - mn);
-      z[h] = z[h] * c0 + zo * c1;
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[h][e] = o[h][e] * c0 + __shfl_xor(o[h][e], x, kWave) * c1;
-      m[h] = mn;
-    }
-  }
-  if (sub == 0) {
-#pragma unroll
-    for (int h = 0; h < GP; ++h) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) red_o[h][cc * E + e] = o[h][e];
-      if (cc == 0) {
-        red_m[h] = m[h];
-        red_z[h] = z[h];
-      }
-    }
-  }
-}
+// Workgroups per CU, and waves per SIMD, as many as registers and LDS allow.  All workgroups of a launch are at work at
+// once, each on one share, and every CU has equally many of them: 512 workgroups of which three fit a CU were spread unevenly
+// (64 requests, 435 MB: 95 us against 86 with 768), and with two or three rounds of shorter shares the workgroups' searches
+// and the joins cost more than the evener end gained (104 and 111 us against 99).
+constexpr int groups_per_cu(int d, int gp) { return d == 64 ? 4 : (gp == 16 ? 2 : 3); }
+constexpr int kCus = 256;
 
-template <int D, int GP, bool FP8>
-__device__ __forceinline__ void attend_matrix(const PagedArgs& a, int r, int head, const int32_t* table, int u0, int u1, int len,
-                                              float (&red_o)[GP][D], float (&red_m)[GP], float (&red_z)[GP]) {
-  constexpr int PE = D / 16;
-  const int lane = threadIdx.x & 63, c = lane & 15, grp = lane >> 4;
-  uint4 qp[D / 32];
-#pragma unroll
-  for (int k = 0; k < D / 32; ++k) {
-    qp[k] = make_uint4(0u, 0u, 0u, 0u);
-    // the elements that the key's loads bring (16 bytes of codes are two k-steps)
-    const int e0 = FP8 ? 64 * (k / 2) + 16 * grp + 8 * (k & 1) : 32 * k + 8 * grp;
-    if (c % GP < a.G) qp[k] = *reinterpret_cast<const uint4*>(a.q + r * a.q_stride + ((size_t)(head * a.G + c % GP) * D + e0) * 2);
-  }
-  AttState<D> st;
-  st.m = kLeast;
-  st.z = 0.f;
-#pragma unroll
-  for (int j = 0; j < PE; ++j) st.acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  attend_units<D, GP, FP8>(st, qp, a, table, head, u0, u1, len);
-
-  const float z = group_sum(st.z);  // the four lane groups saw different keys of the same head
-  if (lane < GP) {
-    red_m[lane] = st.m;
-    red_z[lane] = z;
-  }
-  // product row R = 4 grp + r is part R / GP of head R % GP (parts past the second repeat): the two parts are summed
-#pragma unroll
-  for (int j = 0; j < PE; ++j) {
-    float* dst = &red_o[0][PE * c + j];
-    if constexpr (GP == 16) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) dst[(4 * grp + i) * D] = st.acc[j][i];
-    } else if constexpr (GP == 8) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(st.acc[j][i]), __float_as_uint(st.acc[j][i]), false, false);
-        if (grp < 2) dst[(4 * grp + i) * D] = __uint_as_float(x[0]) + __uint_as_float(x[1]);
-      }
-    } else if constexpr (GP == 4) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(st.acc[j][i]), __float_as_uint(st.acc[j][i]), false, false);
-        if (grp == 0) dst[i * D] = __uint_as_float(x[0]) + __uint_as_float(x[1]);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < GP; ++i)
-        if (grp == 0) dst[i * D] = st.acc[j][i] + st.acc[j][GP + i];
-    }
-  }
+template <typename T>
+__device__ __forceinline__ void write_out(const PagedArgs& a, int pair, int h, int column, int D, float o, float z) {
+  const int r = pair / a.Hkv, head = pair - r * a.Hkv;
+  // (no weight at all, as where every page is missing: zeros)
+  store_elem(a.out + r * a.out_stride + ((size_t)(head * a.G + h) * D + column) * sizeof(T), z == 0.f ? 0.f : o / z, T{});
 }
 
 // grid: groups_per_cu workgroups for every CU, or fewer (a share of kMinUnits units for each of the most that there can be).
 template <typename T, int D, int GP, bool FP8>
-__global__ void __launch_bounds__(kAttThreads, (groups_per_cu(sizeof(T), D, GP))) paged_attention_kernel(PagedArgs a) {
-  __shared__ float red_o[kAttWaves][GP][D];
-  __shared__ float red_m[kAttWaves][GP], red_z[kAttWaves][GP];
+__global__ void __launch_bounds__(kAttThreads, (groups_per_cu(D, GP))) paged_attention_kernel(PagedArgs a) {
+  using At = Attend<T, D, GP, FP8>;
+  __shared__ float red_o[kAttWaves][2][GP][D];
+  __shared__ float red_m[kAttWaves][2][GP], red_z[kAttWaves][2][GP];
+  __shared__ WavePiece pieces[kAttWaves][2];
   const int id = blockIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  auto units = [&](int r) { return (row_len(a, r) + kUnit - 1) / kUnit; };
-  long long all = 0, shares = 0, beg = 0, end = 0;
-  const RowOfUnit at = locate_row(a.R, a.Hkv, units, [&](long long total) {
-    all = total;
-    shares = min((total + kMinUnits - 1) / kMinUnits, (long long)gridDim.x);
-    if (id < shares) {
-      beg = total * id / shares;
-      end = total * (id + 1) / shares;
-    }
-    return beg < end ? beg : -1ll;
-  });
-  int2 cut = make_int2(0, 0);
+  auto units = [&](int r) { return (row_len(a, r) + At::kUnit - 1) / At::kUnit; };
+  Shares cut_in(1, 1);
+  unsigned share = 0, size = 0;   // its first unit, its units
+  auto part = [&](int w) { return share + (unsigned)((unsigned long long)size * w / kAttWaves); };
+  const RowOfUnit at = locate_row(
+      a.R, a.Hkv, units,
+      [&](unsigned total) {
+        const unsigned shares = min((total + kMinUnits - 1) / kMinUnits, gridDim.x);
+        if (id >= (int)shares) return;
+        cut_in = Shares(total, shares);
+        share = cut_in.first(id);
+        size = cut_in.first(id + 1) - share;
+      },
+      [&](int w) { return part(w) < part(w + 1) ? part(w) : ~0u; });
+  unsigned beg = part(wave);
+  const unsigned end = part(wave + 1);
+  if ((threadIdx.x & 63) < 2) pieces[wave][threadIdx.x & 63].there = false;
   if (at.row >= 0) {
-    int r = at.row, len = row_len(a, r), n = at.size;
-    int head = (int)((beg - at.first) / n), u = (int)((beg - at.first) - (long long)head * n);
+    int r = at.row, n = at.size;
+    int head = (int)((beg - at.first) / (unsigned)n), u = (int)(beg - at.first) - head * n;
     while (true) {
-      const int take = (int)min((long long)(n - u), end - beg);
-      const bool whole = take == n;
-      const int32_t* table = a.table + r * a.table_stride;
-      if constexpr (sizeof(T) == 4) attend_f32<D, GP>(a, r, head, table, u, u + take, len, red_o[wave], red_m[wave], red_z[wave]);
-      else attend_matrix<D, GP, FP8>(a, r, head, table, u, u + take, len, red_o[wave], red_m[wave], red_z[wave]);
-      __syncthreads();
-      // a share has at most one piece that goes on from the share before (slot 0) and one that begins here and goes on (1)
-      write_piece<T, GP, D>(a, whole, 2 * id + (u == 0 ? 1 : 0), r, head, red_o, red_m, red_z);
+      const int take = min(n - u, (int)(end - beg));
+      At st;
+      st.begin(a, r, head);
+      st.units(a, a.table + r * a.table_stride, head, u, u + take, row_len(a, r));
       beg += take;
-      if (!whole && u == 0) {
-        // the last unit's share is the largest s with all * s / shares <= its number
-        const long long last = beg + (n - take) - 1;
-        cut = make_int2(r * a.Hkv + head, (int)(((last + 1) * shares - 1) / all) - id);
+      const int pair = r * a.Hkv + head, slot = u == 0 ? 1 : 0;
+      st.put(red_o[wave][slot], red_m[wave][slot], red_z[wave][slot]);
+      if (take == n) {
+        // (the wave's own LDS: its writes are seen by itself in order; slot 1 is not in use before the last piece)
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        for (int i = threadIdx.x & 63; i < a.G * D; i += 64)
+          write_out<T>(a, pair, i / D, i % D, D, red_o[wave][1][i / D][i % D], red_z[wave][1][i / D]);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      } else if ((threadIdx.x & 63) == 0) {
+        pieces[wave][slot] = WavePiece{pair, (int)cut_in.share_of(beg + (n - u - take) - 1) - id, true, u + take == n};
       }
       if (beg >= end) break;
-      __syncthreads();
       u = 0;
       if (++head == a.Hkv) {
         head = 0;
-        do len = row_len(a, ++r); while (len == 0);   // (beg < end: there is another row with positions)
-        n = (len + kUnit - 1) / kUnit;
+        do n = units(++r); while (n == 0);   // (beg < end: there is another row with positions)
       }
     }
+  }
+  __syncthreads();
+  // The pieces of one pair after the other: a slot 0 that no slot 1 precedes goes on from the share before; every slot 1
+  // begins a pair; the slots 0 of the waves behind go on with it until it ends.
+  int2 cut = make_int2(0, 0);
+  unsigned there0 = 0, there1 = 0, ends0 = 0;   // bit w: wave w
+#pragma unroll
+  for (int w = 0; w < kAttWaves; ++w) {
+    there0 |= pieces[w][0].there ? 1u << w : 0u;
+    there1 |= pieces[w][1].there ? 1u << w : 0u;
+    ends0 |= pieces[w][0].there && pieces[w][0].ends ? 1u << w : 0u;
+  }
+  there0 = __builtin_amdgcn_readfirstlane(there0);
+  there1 = __builtin_amdgcn_readfirstlane(there1);
+  ends0 = __builtin_amdgcn_readfirstlane(ends0);
+  unsigned todo = there1;                       // pairs that begin here ...
+  int slot = 1, w0 = there0 ? __builtin_ctz(there0) : 0;
+  if (there0 && (there1 & ((1u << w0) - 1u)) == 0u) slot = 0;   // ... after the one that goes on from before
+  while (slot == 0 || todo != 0u) {
+    if (slot == 1) w0 = __builtin_ctz(todo);
+    // the waves behind that have a piece of the same pair
+    unsigned more = there0 & ~((2u << w0) - 1u);
+    const unsigned last = ends0 & more;
+    bool ends = slot == 0 && ((ends0 >> w0) & 1u) != 0u;
+    if (ends) {
+      more = 0u;
+    } else if (last != 0u) {
+      ends = true;
+      more &= (2u << __builtin_ctz(last)) - 1u;
+    }
+    const WavePiece first = pieces[w0][slot];
+    for (int i = threadIdx.x; i < a.G * D; i += kAttThreads) {
+      const int h = i / D, j = i - h * D;
+      float m[kAttWaves], mn = red_m[w0][slot][h];
+      const float m0 = mn;
+#pragma unroll
+      for (int w = 1; w < kAttWaves; ++w) {
+        m[w] = red_m[w][0][h];
+        mn = (more >> w) & 1u ? fmaxf(mn, m[w]) : mn;
+      }
+      float c = __builtin_amdgcn_exp2f(m0 - mn);
+      float zs = red_z[w0][slot][h] * c, os = red_o[w0][slot][h][j] * c;
+#pragma unroll
+      for (int w = 1; w < kAttWaves; ++w) {
+        c = __builtin_amdgcn_exp2f(m[w] - mn);
+        const float z = fmaf(red_z[w][0][h], c, zs), o = fmaf(red_o[w][0][h][j], c, os);
+        zs = (more >> w) & 1u ? z : zs;
+        os = (more >> w) & 1u ? o : os;
+      }
+      if (slot == 1 && ends) {
+        write_out<T>(a, first.pair, h, j, D, os, zs);
+      } else {
+        const size_t to = (size_t)(2 * id + slot) * a.G + h;
+        a.part[to * D + j] = os;
+        if (j == 0) a.part_mz[to] = make_float2(mn, zs);
+      }
+    }
+    if (slot == 1) {
+      if (!ends) cut = make_int2(first.pair, first.shares);
+      todo &= todo - 1u;
+    }
+    slot = 1;
   }
   if (threadIdx.x == 0) a.cut[id] = cut;
   // rows without positions, dealt to all workgroups
@@ -540,15 +525,15 @@ __global__ void __launch_bounds__(kAttThreads, (groups_per_cu(sizeof(T), D, GP))
       for (int i = threadIdx.x; i < a.Hq * D; i += kAttThreads) store_elem(a.out + r * a.out_stride + (size_t)i * sizeof(T), 0.f, T{});
 }
 
-// grid (workgroups of the first kernel, G): joins the pieces of the (row, kv head) that share blockIdx.x cuts, one query
-// head each.  Four columns per thread, kJoinLanes pieces side by side and eight of each on their way together: a request cut
-// into 128 pieces takes two rounds.  768 shares of seven heads, most of them cut in two or three: 4.3 us; three long fp32
-// requests cut into 128 pieces per head: 6.7 us (half as many pieces side by side 5.5 and 9.5; one column per thread, two
-// pieces side by side 5 and 10).
-constexpr int kJoinLanes = 8;
+// grid (workgroups of the first kernel, G), 256 threads: joins the pieces of the (row, kv head) that share blockIdx.x cuts, one
+// query head each.  Four columns per thread, kLanes pieces side by side and eight of each on their way together: a request
+// cut into 128 pieces takes two rounds, one of 64 columns per row one.  768 shares of seven heads, most of them cut in two or
+// three: 4.3 us; three long fp32 requests cut into 128 pieces per head: 6.3 us with eight pieces side by side (half as many:
+// 9.5 us; one column per thread, two pieces side by side: 10).
+constexpr int kJoinThreads = 256;
 template <typename T, int D>
-__global__ void __launch_bounds__(kJoinLanes * D / 4) paged_join_kernel(PagedArgs a) {
-  constexpr int Q = D / 4, U = 8;
+__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a) {
+  constexpr int Q = D / 4, kJoinLanes = kJoinThreads / Q, U = 8;
   __shared__ float4 lds_o[kJoinLanes][Q];
   __shared__ float lds_m[kJoinLanes], lds_z[kJoinLanes];
   const int id = blockIdx.x, h = blockIdx.y, j = threadIdx.x % Q, lane = threadIdx.x / Q;
@@ -634,17 +619,18 @@ static meda_status make_paged_plan(const meda_page_pool* pool, const meda_paged_
   if (st != MEDA_OK) return st;
   const int G = p->n_q_heads / pool->n_kv_heads;
   const int64_t most = (int64_t)p->max_blocks * pool->page_size;
-  if (G > kMaxGroup || p->n_rows > 65536 || most > (1 << 29) || most * pool->n_kv_heads > (1ll << 34)) return MEDA_ERR_UNSUPPORTED;
-  if ((int64_t)p->n_rows * pool->n_kv_heads > INT32_MAX) return MEDA_ERR_UNSUPPORTED;
   const int elt = dtype_bytes(p->dtype);
+  if (G > kMaxGroup || p->n_rows > 65536 || most > (1 << 29)) return MEDA_ERR_UNSUPPORTED;
+  if (!few_units(p->n_rows, most, pool->n_kv_heads, unit_positions(elt))) return MEDA_ERR_UNSUPPORTED;
+  if ((int64_t)p->n_rows * pool->n_kv_heads > INT32_MAX) return MEDA_ERR_UNSUPPORTED;
   const int64_t row = (int64_t)p->n_q_heads * pool->head_dim, far = 1ll << 40;
   if ((p->q_stride && p->q_stride < row) || (p->out_stride && p->out_stride < row) || (p->table_stride && p->table_stride < p->max_blocks))
     return MEDA_ERR_INVALID_ARG;
   if (p->q_stride * elt % 16 || p->out_stride * elt % 16) return MEDA_ERR_INVALID_ARG;
   if (p->q_stride > far || p->out_stride > far || p->table_stride > far || p->len_stride > far) return MEDA_ERR_UNSUPPORTED;
-  const int64_t units = (most + kUnit - 1) / kUnit * pool->n_kv_heads;     // of one row, at most
+  const int64_t unit = unit_positions(elt), units = (most + unit - 1) / unit * pool->n_kv_heads;   // of one row, at most
   pl->GP = G <= 1 ? 1 : (G <= 2 ? 2 : (G <= 4 ? 4 : (G <= 8 ? 8 : 16)));
-  const int64_t most_groups = kCus * groups_per_cu(elt, pool->head_dim, pl->GP);
+  const int64_t most_groups = kCus * groups_per_cu(pool->head_dim, pl->GP);
   const int64_t shares = units > most_groups * kMinUnits ? most_groups : (units * p->n_rows + kMinUnits - 1) / kMinUnits;
   pl->groups = (int)(shares < most_groups ? shares : most_groups);
   pl->part_bytes = ((size_t)2 * pl->groups * G * pool->head_dim * sizeof(float) + 255) / 256 * 256;
@@ -658,7 +644,7 @@ static hipError_t launch_paged(const PagedPlan& pl, const PagedArgs& a, hipStrea
   hipLaunchKernelGGL((paged_attention_kernel<T, D, GP, FP8>), dim3(pl.groups), dim3(kAttThreads), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(pl.groups, a.G), dim3(kJoinLanes * D / 4), 0, s, a);
+  hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(pl.groups, a.G), dim3(kJoinThreads), 0, s, a);
   return hipGetLastError();
 }
 template <typename T, int D, bool FP8>

@@ -48,19 +48,22 @@ __global__ void __launch_bounds__(kLocateThreads) paged_store_kernel(StoreArgs a
   const int lane = threadIdx.x & 63, sub = lane / LPR, cc = lane - sub * LPR;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   auto pieces = [&](int r) { return (stored_rows(a, r) + kPiece - 1) / kPiece; };
-  long long beg = 0, end = 0;
-  const RowOfUnit at = locate_row(a.R, a.pool.Hkv, pieces, [&](long long total) {
-    beg = total * blockIdx.x / gridDim.x;
-    end = total * (blockIdx.x + 1) / gridDim.x;
-    return beg < end ? beg : -1ll;
-  });
+  unsigned beg = 0, end = 0;
+  const RowOfUnit at = locate_row(
+      a.R, a.pool.Hkv, pieces,
+      [&](unsigned total) {
+        const Shares shares(total, gridDim.x);
+        beg = shares.first(blockIdx.x);
+        end = shares.first(blockIdx.x + 1);
+      },
+      [&](int w) { return beg + w < end ? beg + w : ~0u; });
   if (at.row < 0) return;
   int r = at.row;
-  long long first = at.first;                 // number of row r's first piece
+  unsigned first = at.first;                  // number of row r's first piece
   int rows = stored_rows(a, r), per_head = at.size;
-  for (long long u = beg + wave; u < end; u += kLocateThreads / 64) {
-    while (u >= first + (long long)per_head * a.pool.Hkv) {   // (u < end: there is such a row)
-      first += (long long)per_head * a.pool.Hkv;
+  for (unsigned u = beg + wave; u < end; u += kLocateThreads / 64) {
+    while (u >= first + (unsigned)per_head * a.pool.Hkv) {   // (u < end: there is such a row)
+      first += (unsigned)per_head * a.pool.Hkv;
       ++r;
       rows = stored_rows(a, r);
       per_head = (rows + kPiece - 1) / kPiece;
@@ -136,7 +139,7 @@ meda_status meda_paged_store(const meda_page_pool* pool, const meda_store_params
   st = check_types(p.dtype, pool->dtype);
   if (st != MEDA_OK) return st;
   if ((int64_t)p.n_seqs * p.n_layers > 65536 || (int64_t)p.max_blocks * pool->page_size > (1 << 29)) return MEDA_ERR_UNSUPPORTED;
-  if ((int64_t)p.max_blocks * pool->page_size * pool->n_kv_heads > (1ll << 34) || p.n_src_rows > (1ll << 40)) return MEDA_ERR_UNSUPPORTED;
+  if (!few_units((int64_t)p.n_seqs * p.n_layers, (int64_t)p.max_blocks * pool->page_size, pool->n_kv_heads, kPiece) || p.n_src_rows > (1ll << 40)) return MEDA_ERR_UNSUPPORTED;
   if (p.table_stride && p.table_stride < p.max_blocks) return MEDA_ERR_INVALID_ARG;
   if (!k_rows || !v_rows || !layer_len || !layer_off || !lens || !table) return MEDA_ERR_INVALID_ARG;
   if (((uintptr_t)k_rows | (uintptr_t)v_rows) & 15u) return MEDA_ERR_INVALID_ARG;
