@@ -32,7 +32,7 @@ struct PagedArgs {
   const int32_t* table;
   const int32_t* lens;
   float* part;             // [2 * groups][G][d]: value sums of the pieces
-  float2* part_mz;         // [2 * groups][G]: their maximum (base-2 logits) and normaliser
+  float2* part_mz;         // [2 * groups][G]: their maximum (unscaled logits) and normaliser
   int2* cut;               // [groups]: the (row, kv head) that begins in the share and goes on behind it, as
                            // (row * Hkv + head, shares it reaches into); (0, 0): none
   long long q_stride, out_stride;   // bytes
@@ -48,6 +48,11 @@ __device__ __forceinline__ int row_len(const PagedArgs& a, int r) {
 // A maximum starts at the least finite number, not at -infinity: every finite logit replaces or equals it, a logit of
 // -infinity has the weight exp2(-inf) = 0 under it, and differences of maxima are never inf - inf.
 constexpr float kLeast = -__FLT_MAX__;
+// The weight of logit x under maximum `top`.  Logits and maxima are kept unscaled: the difference of two near ones is exact,
+// and that of a maximum and itself is zero, however large they are.
+__device__ __forceinline__ float weight_under(float x, float top, float scale_log2) {
+  return __builtin_amdgcn_exp2f((x - top) * scale_log2);
+}
 
 // The pages of the 64 / BLOCKS units from u on: lane BLOCKS i + b holds that of block b of the i-th.  One load for many
 // steps: a load of its own in every step would have to be waited for, and with it, as loads come back in order, for all
@@ -183,15 +188,22 @@ struct Attend {
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b) {
       f32x4_t s4 = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      if constexpr (F32) {
+        // four sums of d / 4 products instead of one of d: half the rounding error
+        f32x4_t x4 = s4, y4 = s4, z4 = s4, w4 = s4;
 #pragma unroll
-      for (int k = 0; k < QV; ++k) {
-        if constexpr (F32) {
+        for (int k = 0; k < QV; ++k) {
           const uint4 x = rows.k[b][k], y = q[k];
-          s4 = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.x), __uint_as_float(y.x), s4, 0, 0, 0);
-          s4 = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.y), __uint_as_float(y.y), s4, 0, 0, 0);
-          s4 = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.z), __uint_as_float(y.z), s4, 0, 0, 0);
-          s4 = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.w), __uint_as_float(y.w), s4, 0, 0, 0);
-        } else {
+          x4 = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.x), __uint_as_float(y.x), x4, 0, 0, 0);
+          y4 = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.y), __uint_as_float(y.y), y4, 0, 0, 0);
+          z4 = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.z), __uint_as_float(y.z), z4, 0, 0, 0);
+          w4 = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.w), __uint_as_float(y.w), w4, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s4[i] = (x4[i] + y4[i]) + (z4[i] + w4[i]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < QV; ++k) {
           uint4 x;
           if constexpr (FP8) x = e4m3x8_to_bf16x8((k & 1) ? make_uint2(rows.k[b][k / 2].z, rows.k[b][k / 2].w) : make_uint2(rows.k[b][k / 2].x, rows.k[b][k / 2].y));
           else x = rows.k[b][k];
@@ -209,13 +221,13 @@ struct Attend {
     float sk[8], sv[8];
     bool in[kKeys];
     if constexpr (FP8) {
-      row_broadcast<0>(rows.scale * a.scale_log2, sk);
+      row_broadcast<0>(rows.scale, sk);
       row_broadcast<8>(rows.scale, sv);
     }
     float bm = kLeast;
 #pragma unroll
     for (int e = 0; e < kKeys; ++e) {
-      t[e] *= FP8 ? sk[e] : a.scale_log2;
+      if constexpr (FP8) t[e] *= sk[e];
       if constexpr (MASKED) {
         in[e] = up.ok[e >> 2] && pos + kBlock * (e >> 2) + 4 * g + (e & 3) < len;
         t[e] = in[e] ? t[e] : -INFINITY;
@@ -227,7 +239,7 @@ struct Attend {
     bm = group_max(bm);
     if (__ballot(bm > m) != 0ull) {  // a new maximum of some head: rescale what that head has so far (rare)
       const float mn = fmaxf(m, bm);
-      const float c1 = __builtin_amdgcn_exp2f(m - mn);
+      const float c1 = weight_under(m, mn, a.scale_log2);
       z *= c1;
       m = mn;
 #pragma unroll
@@ -240,7 +252,7 @@ struct Attend {
     float w[kKeys];
 #pragma unroll
     for (int e = 0; e < kKeys; ++e) {
-      float p = __builtin_amdgcn_exp2f(t[e] - m);
+      float p = weight_under(t[e], m, a.scale_log2);
       w[e] = FP8 ? fmaf(p, sv[e], 0.f) : p;  // the sum takes the sign of a zero
       if constexpr (MASKED) {
         p = in[e] ? p : 0.f;
@@ -495,11 +507,11 @@ __global__ void __launch_bounds__(kAttThreads, (groups_per_cu(D, GP))) paged_att
         m[w] = red_m[w][0][h];
         mn = (more >> w) & 1u ? fmaxf(mn, m[w]) : mn;
       }
-      float c = __builtin_amdgcn_exp2f(m0 - mn);
+      float c = weight_under(m0, mn, a.scale_log2);
       float zs = red_z[w0][slot][h] * c, os = red_o[w0][slot][h][j] * c;
 #pragma unroll
       for (int w = 1; w < kAttWaves; ++w) {
-        c = __builtin_amdgcn_exp2f(m[w] - mn);
+        c = weight_under(m[w], mn, a.scale_log2);
         const float z = fmaf(red_z[w][0][h], c, zs), o = fmaf(red_o[w][0][h][j], c, os);
         zs = (more >> w) & 1u ? z : zs;
         os = (more >> w) & 1u ? o : os;
@@ -562,13 +574,13 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a) {
     float top = mn;
 #pragma unroll
     for (int u = 0; u < N; ++u) top = fmaxf(top, mz[u].x);   // (a piece that is repeated changes no maximum)
-    const float c0 = __builtin_amdgcn_exp2f(mn - top);
+    const float c0 = weight_under(mn, top, a.scale_log2);
     zs *= c0;
     os.x *= c0; os.y *= c0; os.z *= c0; os.w *= c0;
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const bool in = s0 + u * kJoinLanes < n;
-      const float c = in ? __builtin_amdgcn_exp2f(mz[u].x - top) : 0.f;
+      const float c = in ? weight_under(mz[u].x, top, a.scale_log2) : 0.f;
       zs = fmaf(in ? mz[u].y : 0.f, c, zs);
       add(os, make_float4(in ? o[u].x : 0.f, in ? o[u].y : 0.f, in ? o[u].z : 0.f, in ? o[u].w : 0.f), c);
     }
@@ -591,7 +603,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a) {
   os = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
   for (int w = 0; w < kJoinLanes; ++w) {
-    const float c = __builtin_amdgcn_exp2f(lds_m[w] - mn);
+    const float c = weight_under(lds_m[w], mn, a.scale_log2);
     zs = fmaf(lds_z[w], c, zs);
     add(os, lds_o[w][j], c);
   }
