@@ -255,6 +255,7 @@ meda_status meda_decode_attention_fp8(const meda_decode_params* params, const vo
  * skips its positions, writers write nothing there), a slot outside [0, n_pages * page_size) is skipped, a length is
  * clamped to [0, max_blocks * page_size].  What lies behind a row's last position is never used and never written.
  * Pages that two rows of one call write to, or slots that occur twice in one call, hold either value afterwards.
+ * The current device of the calling thread is that of hip_stream; calls that share a workspace must not overlap.
  */
 typedef struct {
   int64_t n_pages;     /* pages in the pool, 1 .. 2^31 - 1                                              */
@@ -287,7 +288,7 @@ typedef struct {
  *   granted     [R] int32: m, 0 for a refused row, -1 for an ended one; may be NULL
  *   workspace   256-byte aligned, meda_page_update_workspace_bytes(n_rows) bytes
  * A fresh pool is free_ring = 0 .. n_pages - 1, free_state = {0, n_pages}, lens = 0.  No page may be held twice.
- * lens and lens_out, free_state and free_state_out are the same array or do not overlap.
+ * Apart from lens_out = lens and free_state_out = free_state no array that is written overlaps another one.
  */
 typedef struct {
   int64_t n_pages;     /* 1 .. 2^31 - 1                                                                 */
@@ -310,7 +311,8 @@ meda_status meda_page_update(const meda_page_params* params, const int32_t* lens
  * q_out = dL/dq).  Angles are reduced in 64 bits, the turn is computed in fp32 and rounded once.
  *   q, q_out, k, k_out   token t, head h at t * stride[0] + h * stride[1] (elements; the head_dim elements of a row are
  *                        contiguous).  Any order: token-major projections in, [H][T][d] as meda_compress reads it out.
- *                        An output may be its input (same pointer and strides), otherwise they do not overlap.
+ *                        An output may be its input (same pointer and strides), otherwise it overlaps neither input nor
+ *                        the other output; no two of its rows share memory.
  *                        k, k_out may be NULL with n_k_heads = 0, q and q_out with n_q_heads = 0.
  *   positions            [n_axes][n_tokens] int32, an axis every pos_stride elements (0 = n_tokens)
  *   inv_freq             [rot_dim / 2] double;  axis [rot_dim / 2] uint8, may be NULL with one axis (an axis number past

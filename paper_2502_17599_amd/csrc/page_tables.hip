@@ -252,10 +252,18 @@ meda_status meda_page_update(const meda_page_params* params, const int32_t* lens
   const uintptr_t words = (uintptr_t)lens | (uintptr_t)n_new | (uintptr_t)table | (uintptr_t)free_ring | (uintptr_t)lens_out | (uintptr_t)granted;
   const uintptr_t longs = (uintptr_t)free_state | (uintptr_t)free_state_out | (uintptr_t)slots;
   if ((words & 3u) || (longs & 7u)) return MEDA_ERR_INVALID_ARG;
-  // the same array or none of it in common
-  const intptr_t dl = (intptr_t)lens_out - (intptr_t)lens, ds = (intptr_t)free_state_out - (intptr_t)free_state;
-  const intptr_t nl = (intptr_t)p.n_rows * 4;
-  if ((dl != 0 && dl < nl && dl > -nl) || (ds != 0 && ds < 16 && ds > -16)) return MEDA_ERR_INVALID_ARG;
+  // What is written overlaps nothing else that the call reads or writes; lens_out and free_state_out may be lens and free_state.
+  struct Range { const void* at; uint64_t bytes; };
+  const uint64_t R = (uint64_t)p.n_rows;
+  const Range all[] = {{table, R * p.max_blocks * 4}, {free_ring, (uint64_t)p.n_pages * 4}, {lens_out, R * 4}, {free_state_out, 16},
+                       {p.max_new > 0 ? slots : nullptr, R * p.max_new * 8}, {granted, R * 4},
+                       {lens, R * 4}, {n_new, R * 4}, {free_state, 16}};
+  for (int x = 0; x < 6; ++x)
+    for (int y = x + 1; y < 9; ++y) {
+      if (!all[x].at || !all[y].at || (x == 2 && y == 6 && lens_out == lens) || (x == 3 && y == 8 && free_state_out == free_state)) continue;
+      const uintptr_t u = (uintptr_t)all[x].at, v = (uintptr_t)all[y].at;
+      if (u < v + all[y].bytes && v < u + all[x].bytes) return MEDA_ERR_INVALID_ARG;
+    }
   if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < meda_page_update_workspace_bytes(p.n_rows)) return MEDA_ERR_WORKSPACE;
 
   PageUpdate a;

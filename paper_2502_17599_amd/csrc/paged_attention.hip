@@ -1,8 +1,8 @@
 // Attention of one new token per row over its pages: out = Softmax(q K^T / sqrt(d)) V.
 //
 // Every cached key and value is read once and takes 4 * G * d flops per pair (G query heads share a kv head), so the step
-// is bound by HBM where it is long and by latency where it is short.  The work is numbered in units of 32 positions, row
-// after row and kv head after kv head, and cut into contiguous shares of equal size, one per workgroup, on the device:
+// is bound by HBM where it is long and by latency where it is short.  The work is numbered in units of 32 positions (fp32: 16),
+// row after row and kv head after kv head, and cut into contiguous shares of equal size, one per workgroup, on the device:
 // lengths that differ by a factor of a thousand, empty rows and a single long request all fill the chip.  A
 // (row, kv head) that lies in one share is finished by its workgroup; one that is cut leaves, per share, a running maximum,
 // a normaliser and a weighted value sum, which a second kernel joins.
@@ -397,11 +397,11 @@ struct WavePiece {
   bool ends;    // slot 0: the pair ends in this wave
 };
 
-// Workgroups per CU, and waves per SIMD, as many as registers and LDS allow.  All workgroups of a launch are at work at
-// once, each on one share, and every CU has equally many of them: 512 workgroups of which three fit a CU were spread unevenly
-// (64 requests, 435 MB: 95 us against 86 with 768), and with two or three rounds of shorter shares the workgroups' searches
-// and the joins cost more than the evener end gained (104 and 111 us against 99).
-constexpr int groups_per_cu(int d, int gp) { return d == 64 ? 4 : (gp == 16 ? 2 : 3); }
+// Workgroups per CU, and waves per SIMD: three where registers and LDS allow it.  All workgroups of a launch are at work at
+// once, each on one share.  (64 requests, 435 MB: 88 us with two per CU, 86 with three; with two and three rounds of shorter
+// shares 104 and 111 instead of 99, before the pages of many steps were loaded at once: the workgroups' searches and the joins
+// cost more than the evener end gained.  Rows of 64 elements, four per CU: three fp32 requests 41.6 us, three per CU 40.1.)
+constexpr int groups_per_cu(int d, int gp) { return d == 128 && gp == 16 ? 2 : 3; }
 constexpr int kCus = 256;
 
 template <typename T>
@@ -638,8 +638,8 @@ static meda_status make_paged_plan(const meda_page_pool* pool, const meda_paged_
   const int64_t row = (int64_t)p->n_q_heads * pool->head_dim, far = 1ll << 40;
   if ((p->q_stride && p->q_stride < row) || (p->out_stride && p->out_stride < row) || (p->table_stride && p->table_stride < p->max_blocks))
     return MEDA_ERR_INVALID_ARG;
-  if (p->q_stride * elt % 16 || p->out_stride * elt % 16) return MEDA_ERR_INVALID_ARG;
   if (p->q_stride > far || p->out_stride > far || p->table_stride > far || p->len_stride > far) return MEDA_ERR_UNSUPPORTED;
+  if (p->q_stride * elt % 16 || p->out_stride * elt % 16) return MEDA_ERR_INVALID_ARG;
   const int64_t unit = unit_positions(elt), units = (most + unit - 1) / unit * pool->n_kv_heads;   // of one row, at most
   pl->GP = G <= 1 ? 1 : (G <= 2 ? 2 : (G <= 4 ? 4 : (G <= 8 ? 8 : 16)));
   const int64_t most_groups = kCus * groups_per_cu(pool->head_dim, pl->GP);

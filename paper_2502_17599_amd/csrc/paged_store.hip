@@ -141,6 +141,7 @@ meda_status meda_paged_store(const meda_page_pool* pool, const meda_store_params
   if ((int64_t)p.n_seqs * p.n_layers > 65536 || (int64_t)p.max_blocks * pool->page_size > (1 << 29)) return MEDA_ERR_UNSUPPORTED;
   if (!few_units((int64_t)p.n_seqs * p.n_layers, (int64_t)p.max_blocks * pool->page_size, pool->n_kv_heads, kPiece) || p.n_src_rows > (1ll << 40)) return MEDA_ERR_UNSUPPORTED;
   if (p.table_stride && p.table_stride < p.max_blocks) return MEDA_ERR_INVALID_ARG;
+  if (p.table_stride > (1ll << 40) || p.len_stride > (1ll << 40)) return MEDA_ERR_UNSUPPORTED;
   if (!k_rows || !v_rows || !layer_len || !layer_off || !lens || !table) return MEDA_ERR_INVALID_ARG;
   if (((uintptr_t)k_rows | (uintptr_t)v_rows) & 15u) return MEDA_ERR_INVALID_ARG;
   if ((((uintptr_t)layer_len | (uintptr_t)lens | (uintptr_t)table) & 3u) || ((uintptr_t)layer_off & 7u)) return MEDA_ERR_INVALID_ARG;

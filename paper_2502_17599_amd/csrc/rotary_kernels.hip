@@ -175,19 +175,28 @@ static meda_status make_rotation(RotaryPlan* out, const int32_t* positions, cons
                     (flags & MEDA_ROTARY_INTERLEAVED) ? 1 : 0, (flags & MEDA_ROTARY_INVERSE) ? -1.f : 1.f};
   if (rot_dim == 0) return MEDA_OK;
   if (!positions || !inv_freq || (!axis && n_axes > 1) || pos_stride < 0) return MEDA_ERR_INVALID_ARG;
+  if (pos_stride > (1ll << 40)) return MEDA_ERR_UNSUPPORTED;
   if (((uintptr_t)positions & 3u) || ((uintptr_t)inv_freq & 7u)) return MEDA_ERR_INVALID_ARG;
   return MEDA_OK;
 }
 
-// Rows by strides, in elements; false where they cannot be moved in 16-byte pieces.
-static bool make_rows(Rows* r, const void* in, void* out, const int64_t* in_stride, const int64_t* out_stride, int heads, int elt) {
-  *r = Rows{static_cast<const char*>(in), static_cast<char*>(out), in_stride[0] * elt, in_stride[1] * elt,
-            out ? out_stride[0] * elt : 0, out ? out_stride[1] * elt : 0, heads};
-  const int64_t most = 1ll << 45;
+// Rows of d elements by strides, in elements; false where they cannot be moved in 16-byte pieces or where rows that are
+// written share memory.
+static bool make_rows(Rows* r, const void* in, void* out, const int64_t* in_stride, const int64_t* out_stride, int64_t tokens, int heads,
+                      int d, int elt) {
+  const int64_t most = 1ll << 40;
   for (int i = 0; i < 2; ++i) {
     if (in_stride[i] < 0 || in_stride[i] > most || (in_stride[i] * elt) % 16) return false;
     if (out && (out_stride[i] < 0 || out_stride[i] > most || (out_stride[i] * elt) % 16)) return false;
   }
+  if (out) {
+    // the dimension with the shorter stride lies inside a step of the other one
+    const int in_dim = heads > 1 && (tokens <= 1 || out_stride[1] < out_stride[0]) ? 1 : 0;
+    const int64_t n[2] = {tokens, heads}, inner = n[in_dim] > 1 ? out_stride[in_dim] : d, outer = n[1 - in_dim] > 1 ? out_stride[1 - in_dim] : most;
+    if (inner < d || (double)(n[in_dim] - 1) * (double)inner + d > (double)outer) return false;
+  }
+  *r = Rows{static_cast<const char*>(in), static_cast<char*>(out), in_stride[0] * elt, in_stride[1] * elt,
+            out ? out_stride[0] * elt : 0, out ? out_stride[1] * elt : 0, heads};
   return in && !((uintptr_t)in & 15u) && !((uintptr_t)out & 15u);
 }
 
@@ -219,9 +228,9 @@ meda_status meda_rotary(const meda_rotary_params* params, const void* q, const v
   RotaryArgs a{};
   const meda_status sr = make_rotation(&a.plan, positions, inv_freq, axis, p.rot_dim, p.n_axes, p.pos_stride, p.n_tokens, p.flags);
   if (sr != MEDA_OK) return sr;
-  const int elt = dtype_bytes(p.dtype);
-  if (p.n_q_heads > 0 && (!q_out || !make_rows(&a.q, q, q_out, p.q_stride, p.q_out_stride, p.n_q_heads, elt))) return MEDA_ERR_INVALID_ARG;
-  if (p.n_k_heads > 0 && (!k_out || !make_rows(&a.k, k, k_out, p.k_stride, p.k_out_stride, p.n_k_heads, elt))) return MEDA_ERR_INVALID_ARG;
+  const int elt = dtype_bytes(p.dtype), d = p.head_dim;
+  if (p.n_q_heads > 0 && (!q_out || !make_rows(&a.q, q, q_out, p.q_stride, p.q_out_stride, p.n_tokens, p.n_q_heads, d, elt))) return MEDA_ERR_INVALID_ARG;
+  if (p.n_k_heads > 0 && (!k_out || !make_rows(&a.k, k, k_out, p.k_stride, p.k_out_stride, p.n_tokens, p.n_k_heads, d, elt))) return MEDA_ERR_INVALID_ARG;
   a.tokens = p.n_tokens;
   const hipError_t e = launch_rotary_of<kToRows>(p.dtype, p.head_dim, a, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? MEDA_OK : MEDA_ERR_HIP;
@@ -237,6 +246,7 @@ meda_status meda_paged_append(const meda_page_pool* pool, const meda_append_para
   const meda_status sp = read_pool(pool, &a.pool);
   if (sp != MEDA_OK) return sp;
   if (p.n_tokens < 0 || p.n_q_heads < 0 || p.slot_stride < 0) return MEDA_ERR_INVALID_ARG;
+  if (p.slot_stride > (1ll << 40)) return MEDA_ERR_UNSUPPORTED;
   meda_status st = check_types(p.dtype, pool->dtype);
   if (st != MEDA_OK) return st;
   if ((int64_t)p.n_q_heads + 2ll * pool->n_kv_heads > 131070 || p.n_q_heads > 65535 || p.n_tokens > (1ll << 26)) return MEDA_ERR_UNSUPPORTED;
@@ -245,12 +255,12 @@ meda_status meda_paged_append(const meda_page_pool* pool, const meda_append_para
   if (p.n_tokens == 0) return MEDA_OK;
   st = make_rotation(&a.plan, positions, inv_freq, axis, p.rot_dim, p.n_axes, p.pos_stride, p.n_tokens, p.flags);
   if (st != MEDA_OK) return st;
-  const int elt = dtype_bytes(p.dtype);
+  const int elt = dtype_bytes(p.dtype), d = pool->head_dim;
   Rows v_rows{};
   const int64_t none[2] = {0, 0};
-  if (p.n_q_heads > 0 && (!q_out || !make_rows(&a.q, q, q_out, p.q_stride, p.q_out_stride, p.n_q_heads, elt))) return MEDA_ERR_INVALID_ARG;
-  if (!make_rows(&a.k, k, nullptr, p.k_stride, none, pool->n_kv_heads, elt)) return MEDA_ERR_INVALID_ARG;
-  if (!make_rows(&v_rows, v, nullptr, p.v_stride, none, pool->n_kv_heads, elt)) return MEDA_ERR_INVALID_ARG;
+  if (p.n_q_heads > 0 && (!q_out || !make_rows(&a.q, q, q_out, p.q_stride, p.q_out_stride, p.n_tokens, p.n_q_heads, d, elt))) return MEDA_ERR_INVALID_ARG;
+  if (!make_rows(&a.k, k, nullptr, p.k_stride, none, p.n_tokens, pool->n_kv_heads, d, elt)) return MEDA_ERR_INVALID_ARG;
+  if (!make_rows(&v_rows, v, nullptr, p.v_stride, none, p.n_tokens, pool->n_kv_heads, d, elt)) return MEDA_ERR_INVALID_ARG;
   if (!slots || ((uintptr_t)slots & 7u)) return MEDA_ERR_INVALID_ARG;
   a.v = v_rows.in; a.v_token = v_rows.in_token; a.v_head = v_rows.in_head;
   a.slots = slots;

@@ -90,6 +90,9 @@ def test_page_update_refuses(lib):
         assert _update(lib, ptrs={name: FAKE + 2}) == INVALID, name
     assert _update(lib, ptrs=dict(lens_out=FAKE + 4)) == INVALID       # overlaps lens without being it
     assert _update(lib, ptrs=dict(state_out=FAKE + 32768 + 8)) == INVALID
+    for name, at in (("lens_out", FAKE + 4096), ("granted", FAKE), ("granted", FAKE + 4096 + 8), ("slots", FAKE + 8192 + 64),
+                     ("table", FAKE + 16384 + 256), ("state_out", FAKE + 65536)):
+        assert _update(lib, ptrs={name: at}) == INVALID, (name, at)    # written arrays overlap nothing
     assert _update(lib, ws=FAKE + 16) == WORKSPACE and _update(lib, ws=0) == WORKSPACE
     assert _update(lib, ws_bytes=lib.meda_page_update_workspace_bytes(4) - 1) == WORKSPACE
     assert lib.meda_page_update_workspace_bytes(0) == 0 and lib.meda_page_update_workspace_bytes(-3) == 0
@@ -119,6 +122,9 @@ def test_rotary_refuses(lib):
         assert _rotary(lib, ptrs={name: None}) == INVALID, name
     for name, off in (("q", 8), ("k_out", 2), ("positions", 2), ("inv_freq", 4)):
         assert _rotary(lib, ptrs={name: FAKE + off}) == INVALID, name
+    # rows that are written share no memory: a stride of zero, heads or tokens inside each other
+    for out in ((0, 128), (1024, 0), (1024, 64), (512, 128), (128, 512), (640, 128), (128, 639 // 16 * 16)):
+        assert _rotary(lib, dict(q_out_stride=out)) == INVALID, out
     assert lib.meda_rotary(None, *[FAKE] * 7, None) == INVALID
     assert _rotary(lib, dict(n_tokens=0)) == 0 and _rotary(lib, dict(n_q_heads=0, n_k_heads=0)) == 0   # nothing to do
 
