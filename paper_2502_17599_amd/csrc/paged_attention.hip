@@ -537,6 +537,49 @@ __global__ void __launch_bounds__(kAttThreads, (groups_per_cu(D, GP))) paged_att
       for (int i = threadIdx.x; i < a.Hq * D; i += kAttThreads) store_elem(a.out + r * a.out_stride + (size_t)i * sizeof(T), 0.f, T{});
 }
 
+// ---- short tables -----------------------------------------------------------------------------------------------------
+//
+// Where no row can be long, a workgroup per (row, kv head) is enough: no search, no pieces in memory, no second launch.
+// WAVES contiguous parts of the pair's units, added up in LDS.  grid (Hkv, R).
+//
+// A CU takes the rows of a pair in at some 150 GB/s, so a table is short up to kPairBytes of keys and values per pair, and up
+// to kPairPositions where there are too few pairs to keep the chip busy beside (pairs against shares: 2000 rows of up to 300
+// positions 30 and 39 us, 512 pairs of up to 600 23 and 28, 256 pairs of up to 1000 8-bit positions 15 and 18, 8 pairs of 100
+// 6.9 and 9.9; beyond: 128 pairs of up to 1023 20 and 18, 8 pairs of 1023 15 and 10, 8 pairs of 1000 8-bit positions 14 and
+// 11).  Eight waves where every workgroup has a CU to itself, four otherwise (128 pairs of up to 600 13.6 and 14.2 us with
+// eight and four, 2000 pairs of up to 300 51 and 30).
+constexpr int kPairBytes = 320 << 10, kPairPositions = 512, kFewPairs = 64;
+template <typename T, int D, int GP, bool FP8, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, (WAVES == 4 ? groups_per_cu(D, GP) : 2)) paged_pair_kernel(PagedArgs a) {
+  using At = Attend<T, D, GP, FP8>;
+  __shared__ float red_o[WAVES][GP][D];
+  __shared__ float red_m[WAVES][GP], red_z[WAVES][GP];
+  const int head = blockIdx.x, r = blockIdx.y, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int len = __builtin_amdgcn_readfirstlane(row_len(a, r)), n = (len + At::kUnit - 1) / At::kUnit;
+  const int each = (n + WAVES - 1) / WAVES, active = each > 0 ? (n + each - 1) / each : 0;   // waves 0 .. active - 1 have units
+  if (wave < active) {
+    At st;
+    st.begin(a, r, head);
+    st.units(a, a.table + r * a.table_stride, head, wave * each, min((wave + 1) * each, n), len);
+    st.put(red_o[wave], red_m[wave], red_z[wave]);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < a.G * D; i += 64 * WAVES) {
+    const int h = i / D, j = i - h * D;
+    float mn = kLeast, zs = 0.f, os = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) mn = w < active ? fmaxf(mn, red_m[w][h]) : mn;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float c = weight_under(red_m[w][h], mn, a.scale_log2);
+      const float z = fmaf(red_z[w][h], c, zs), o = fmaf(red_o[w][h][j], c, os);
+      zs = w < active ? z : zs;
+      os = w < active ? o : os;
+    }
+    write_out<T>(a, r * a.Hkv + head, h, j, D, os, zs);
+  }
+}
+
 // grid (workgroups of the first kernel, G), 256 threads: joins the pieces of the (row, kv head) that share blockIdx.x cuts, one
 // query head each.  Four columns per thread, kLanes pieces side by side and eight of each on their way together: a request
 // cut into 128 pieces takes two rounds, one of 64 columns per row one.  768 shares of seven heads, most of them cut in two or
@@ -616,6 +659,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a) {
 
 struct PagedPlan {
   int groups, GP;
+  int pair_waves;   // waves of a workgroup per (row, kv head); 0: shares
   size_t part_bytes, mz_bytes, ws_bytes;
 };
 
@@ -645,6 +689,10 @@ static meda_status make_paged_plan(const meda_page_pool* pool, const meda_paged_
   const int64_t most_groups = kCus * groups_per_cu(pool->head_dim, pl->GP);
   const int64_t shares = units > most_groups * kMinUnits ? most_groups : (units * p->n_rows + kMinUnits - 1) / kMinUnits;
   pl->groups = (int)(shares < most_groups ? shares : most_groups);
+  pl->pair_waves = 0;
+  const int64_t pairs = (int64_t)p->n_rows * pool->n_kv_heads;
+  if (most * 2 * pool->head_dim * dtype_bytes(pool->dtype) <= kPairBytes && (pairs > kFewPairs || most <= kPairPositions) && p->n_rows <= 65535)
+    pl->pair_waves = pairs <= kCus ? 8 : 4;
   pl->part_bytes = ((size_t)2 * pl->groups * G * pool->head_dim * sizeof(float) + 255) / 256 * 256;
   pl->mz_bytes = ((size_t)2 * pl->groups * G * sizeof(float2) + 255) / 256 * 256;
   pl->ws_bytes = pl->part_bytes + pl->mz_bytes + ((size_t)pl->groups * sizeof(int2) + 255) / 256 * 256;
@@ -653,6 +701,14 @@ static meda_status make_paged_plan(const meda_page_pool* pool, const meda_paged_
 
 template <typename T, int D, int GP, bool FP8>
 static hipError_t launch_paged(const PagedPlan& pl, const PagedArgs& a, hipStream_t s) {
+  if (pl.pair_waves == 8) {
+    hipLaunchKernelGGL((paged_pair_kernel<T, D, GP, FP8, 8>), dim3(a.Hkv, a.R), dim3(512), 0, s, a);
+    return hipGetLastError();
+  }
+  if (pl.pair_waves == 4) {
+    hipLaunchKernelGGL((paged_pair_kernel<T, D, GP, FP8, 4>), dim3(a.Hkv, a.R), dim3(256), 0, s, a);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL((paged_attention_kernel<T, D, GP, FP8>), dim3(pl.groups), dim3(kAttThreads), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

@@ -40,17 +40,28 @@ def _run(lens, Hq, Hkv, d, cache, page, joint=False, seed=0, scale=0.0, spare=2,
     return pool, table, ln, q, out
 
 
+# Tables that cannot hold long rows are served by a workgroup per row and kv head, wider ones in shares: both are tested.
+WIDE = 2000
+BOTH = pytest.mark.parametrize("wide", [False, True])
+
+
+def _widen(table, wide):
+    return torch.nn.functional.pad(table, (0, WIDE - table.shape[1]), value=-7) if wide else table
+
+
+@BOTH
 @pytest.mark.parametrize("G", [1, 2, 3, 4, 5, 7, 8, 9, 16])
 @pytest.mark.parametrize("cache,d", [("bf16", 128), ("bf16", 64), ("fp8", 128), ("fp8", 64), ("f32", 128), ("f32", 64)])
-def test_groups_and_types(G, cache, d):
-    _run([1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 300, 0, 2], 2 * G, 2, d, cache, 16, seed=G)
+def test_groups_and_types(G, cache, d, wide):
+    _run([1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 300, 0, 2], 2 * G, 2, d, cache, 16, seed=G, width=WIDE if wide else None)
 
 
+@BOTH
 @pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
 @pytest.mark.parametrize("cache", ["bf16", "fp8", "f32"])
-def test_page_sizes_and_ends_inside_a_page(page, cache):
+def test_page_sizes_and_ends_inside_a_page(page, cache, wide):
     lens = [page - 1, page, page + 1, 1, 0, 2 * page - 15, 2 * page + 16, 3 * page + 17]
-    _run(lens, 6, 3, 128 if cache != "f32" else 64, cache, page, joint=cache != "fp8", seed=page)
+    _run(lens, 6, 3, 128 if cache != "f32" else 64, cache, page, joint=cache != "fp8", seed=page, width=WIDE if wide else None)
 
 
 @pytest.mark.parametrize("lens,Hq,Hkv,cache,page", [
@@ -68,22 +79,24 @@ def test_many_rows():
     _run(lens, 4, 2, 64, "bf16", 16, rows=range(0, 1500, 50))
 
 
-def test_all_rows_empty():
+@BOTH
+def test_all_rows_empty(wide):
     import paper_2502_17599_amd as pkg
     pool = make_pool("bf16", 2, 2, 16, 64)
-    table, lens = torch.full((3, 4), -1, dtype=torch.int32, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
-    dec = pkg.PagedDecoder(pool, 3, 4, 4)
+    table, lens = _widen(torch.full((3, 4), -1, dtype=torch.int32, device=DEV), wide), torch.zeros(3, dtype=torch.int32, device=DEV)
+    dec = pkg.PagedDecoder(pool, 3, 4, table.shape[1])
     dec.out.fill_(7.0)
     assert (dec(normal(1, 3, 4, 64, dtype="bf16"), table, lens) == 0).all()
 
 
+@BOTH
 @pytest.mark.parametrize("cache", ["bf16", "fp8", "f32"])
-def test_what_lies_behind_the_end_does_not_count(cache):
+def test_what_lies_behind_the_end_does_not_count(cache, wide):
     """NaN and infinities behind the last position, in pages nobody holds and in their scales; page numbers behind the held
     blocks that name no page; lengths past the table or below zero."""
     import paper_2502_17599_amd as pkg
     lens = [5, 33, 130, 64]
-    pool, table, ln, q, out = _run(lens, 4, 2, 128, cache, 32, seed=3, spare=4)
+    pool, table, ln, q, out = _run(lens, 4, 2, 128, cache, 32, seed=3, spare=4, width=WIDE if wide else None)
     held = np.zeros((pool.n_pages, 32), bool)
     tab = table.cpu().numpy()
     for r, n in enumerate(lens):
@@ -112,8 +125,9 @@ def test_what_lies_behind_the_end_does_not_count(cache):
     _check(zeroed, q, pool, table, over)
 
 
+@BOTH
 @pytest.mark.parametrize("cache", ["bf16", "fp8", "f32"])
-def test_missing_pages_are_left_out(cache):
+def test_missing_pages_are_left_out(cache, wide):
     import paper_2502_17599_amd as pkg
     lens, page = [200, 64, 33, 1, 400], 16
     n_pages = 60
@@ -121,6 +135,7 @@ def test_missing_pages_are_left_out(cache):
     table, ln = make_table(lens, page, n_pages, seed=5)
     table[0, 3] = -1; table[0, 4] = n_pages; table[1, 0] = 2 ** 31 - 1; table[2, 2] = -2 ** 31; table[3, 0] = -1; table[4, 24] = -9
     q = normal(4, 5, 6, 64, dtype="f32" if cache == "f32" else "bf16")
+    table = _widen(table, wide)
     out = pkg.PagedDecoder(pool, 5, 6, table.shape[1])(q, table, ln)
     _check(out, q, pool, table, ln)
     assert (out[3] == 0).all()
@@ -134,42 +149,44 @@ def test_length_past_the_table_is_clamped():
     _check(got, q, pool, table, torch.tensor([64, 64], dtype=torch.int32, device=DEV))
 
 
+@BOTH
 @pytest.mark.parametrize("cache", ["bf16", "f32"])
-def test_extreme_values(cache):
+def test_extreme_values(cache, wide):
     """Logits far apart, all equal, at the bottom of the range; infinite values and keys."""
     import paper_2502_17599_amd as pkg
     dt = DT[cache]
     page, n = 16, 48
     pool = make_pool(cache, 6, 1, page, 64, seed=7)
-    table, lens = make_table([n, n], page, 6, seed=7)
-    tab = table.cpu().numpy()
+    table, lens = make_table([n, n], page, 6, seed=7, width=WIDE if wide else 3)
+    tab, W = table.cpu().numpy(), table.shape[1]
     q = torch.zeros(2, 1, 64, dtype=dt, device=DEV)
-    out = pkg.PagedDecoder(pool, 2, 1, 3)(q[:, :1], table[:, :3], lens)
+    out = pkg.PagedDecoder(pool, 2, 1, W)(q, table, lens)
     _check(out, q, pool, table, lens)                                    # equal logits: the mean
     q[0, 0, 0] = 1e30
     pool.k_pages[..., 0] = -1e8
-    _check(pkg.PagedDecoder(pool, 2, 1, 3)(q, table, lens), q, pool, table, lens)     # every logit near -1e37, all equal
+    _check(pkg.PagedDecoder(pool, 2, 1, W)(q, table, lens), q, pool, table, lens)     # every logit near -1e37, all equal
     pool.k_pages[tab[0, 1], 0, 5, 0] = 1.0
-    got = pkg.PagedDecoder(pool, 2, 1, 3)(q, table, lens)
+    got = pkg.PagedDecoder(pool, 2, 1, W)(q, table, lens)
     assert torch.equal(got[0, 0], pool.v_pages[tab[0, 1], 0, 5])                       # one key takes everything
     pool.k_pages[tab[0, 0], 0, :, 0] = float("-inf")                                   # no weight at all
-    assert torch.equal(pkg.PagedDecoder(pool, 2, 1, 3)(q, table, lens)[0, 0], pool.v_pages[tab[0, 1], 0, 5])
+    assert torch.equal(pkg.PagedDecoder(pool, 2, 1, W)(q, table, lens)[0, 0], pool.v_pages[tab[0, 1], 0, 5])
     q[1] = normal(8, 1, 64, dtype=cache)
     pool.k_pages[..., 0] = 0
     pool.v_pages[tab[1, 0], 0, 3, 10] = float("inf")
     pool.v_pages[tab[1, 2], 0, 3, 11] = float("-inf")
-    got = pkg.PagedDecoder(pool, 2, 1, 3)(q, table, lens)[1, 0]
+    got = pkg.PagedDecoder(pool, 2, 1, W)(q, table, lens)[1, 0]
     assert got[10] == float("inf") and got[11] == float("-inf") and torch.isfinite(got[torch.arange(64, device=DEV) // 2 != 5]).all()
     pool.k_pages[tab[1, 1], 0, 2, 7] = float("nan")
-    assert torch.isnan(pkg.PagedDecoder(pool, 2, 1, 3)(q, table, lens)[1]).all()
+    assert torch.isnan(pkg.PagedDecoder(pool, 2, 1, W)(q, table, lens)[1]).all()
 
 
-def test_strides_and_outputs():
+@BOTH
+def test_strides_and_outputs(wide):
     """Rows of one layer out of a table of several, queries inside a fused projection, an output of the caller's."""
     import paper_2502_17599_amd as pkg
     L, N, page = 3, 4, 32
     lens = [20, 33, 0, 64, 7, 90, 100, 1, 65, 31, 32, 128]
-    pool, table, ln, q, out = _run(lens, 4, 2, 128, "bf16", page, seed=11)
+    pool, table, ln, q, out = _run(lens, 4, 2, 128, "bf16", page, seed=11, width=WIDE if wide else None)
     for l in range(L):
         dec = pkg.PagedDecoder(pool, N, 4, table.shape[1])
         qkv = torch.full((N, 8, 128), 9.0, dtype=torch.bfloat16, device=DEV)
@@ -237,3 +254,37 @@ def test_refusals():
             pkg.PagedDecoder(*args)
     with pytest.raises(pkg.MedaError):
         pkg.PagedDecoder(pool, 2, 4, W, softmax_scale=-1.0)
+
+
+@pytest.mark.parametrize("width", [None, 4000])
+@pytest.mark.parametrize("cache,G", [("bf16", 4), ("bf16", 16), ("fp8", 7), ("f32", 5)])
+def test_short_rows_in_short_and_wide_tables(width, cache, G):
+    """The same rows where the table says that they are short (a workgroup per row and kv head) and where it could hold long
+    ones (shares): rows of one wave's units, of all waves', and none."""
+    lens = [0, 1, 16, 31, 32, 33, 64, 100, 128, 129, 160, 200, 255, 256, 257, 300] * 3
+    _run(lens, 2 * G, 2, 128, cache, 16, seed=G, width=width, rows=range(16))
+    _run(lens[5:10], 3 * G, 3, 64, cache, 16, seed=G + 1, width=width)     # few pairs
+
+
+def test_many_waves_in_one_pair_and_one_wave_over_many_pairs():
+    """Shares that begin and end inside pairs, pairs that end inside a wave's part, pairs of one unit."""
+    for seed, lens in ((1, [33, 1, 700, 5, 0, 0, 64, 2100, 31, 1, 1, 1, 900, 12]), (2, [1] * 300 + [5000] + [1] * 300), (3, [17] * 1000), (4, [4096, 4095, 1, 4097])):
+        _run(lens, 4, 2, 64, "bf16", 16, seed=seed, width=512, rows=range(0, len(lens), max(1, len(lens) // 40)))
+        _run(lens, 4, 2, 64, "f32", 16, seed=seed, width=512, rows=range(0, len(lens), max(1, len(lens) // 40)))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp8", "f32"])
+def test_long_walks_of_one_wave(cache):
+    """So many positions that every wave walks over more units than one load of page numbers covers.  The rows read the same
+    few pages over and over (pages may be shared), each in an order of its own; some of their blocks name no page."""
+    import paper_2502_17599_amd as pkg
+    R, Hkv, page, n_pages, width = 64, 2, 16, 300, 3750
+    pool = make_pool(cache, n_pages, Hkv, page, 64, seed=21)
+    rng = np.random.default_rng(22)
+    table = rng.integers(0, n_pages, size=(R, width)).astype(np.int32)
+    table[3, 1000] = -1; table[5, 3000:3010] = n_pages; table[40, 17] = 2 ** 31 - 1
+    lens = rng.integers(55000, width * page + 1, size=R).astype(np.int32)
+    lens[7] = width * page
+    t, n = torch.from_numpy(table).to(DEV), torch.from_numpy(lens).to(DEV)
+    q = normal(23, R, 2 * Hkv, 64, dtype="f32" if cache == "f32" else "bf16")
+    _check(pkg.PagedDecoder(pool, R, 2 * Hkv, width)(q, t, n), q, pool, t, n, rows=(0, 3, 5, 7, 31, 40, 63))
