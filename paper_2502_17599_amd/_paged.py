@@ -31,6 +31,14 @@ def _call(fn, device: int, stream, *args):
         _check(status)
 
 
+def _empty(shape, dtype, device, stream):
+    """New memory for a call on ``stream``: taken from that stream's memory, which nothing else on its way uses."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 # A call of a kind that was checked before (the same shapes, strides, types and devices) is not checked again: half of the
 # time of a small call went into it.  What an entry holds depends on nothing else, addresses least of all.
 _checked: dict = {}
@@ -184,9 +192,9 @@ def meda_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Ten
         plan = _remember(key, _plan_rotary(q, k, positions, rope, q_out, k_out, inverse))
     params, dev, new_q, new_k, ext = plan
     if new_q is not None:
-        q_out = torch.empty(new_q, dtype=q.dtype, device=q.device)
+        q_out = _empty(new_q, q.dtype, q.device, stream)
     if new_k is not None:
-        k_out = torch.empty(new_k, dtype=k.dtype, device=k.device)
+        k_out = _empty(new_k, k.dtype, k.device, stream)
     pq, pk, po, pko = q.data_ptr(), _p(k), q_out.data_ptr(), _p(k_out)
     for name, out, a, n in (("q_out", q_out, po, ext[2]), ("k_out", k_out, pko, ext[3])):
         if out is not None:
@@ -244,7 +252,7 @@ def meda_paged_append(pool: PagePool, k: torch.Tensor, v: torch.Tensor, slots: t
         plan = _remember(key, _plan_append(pool, k, v, slots, q, positions, rope, q_out))
     params, new_q, ext = plan
     if new_q is not None:
-        q_out = torch.empty(new_q, dtype=q.dtype, device=q.device)
+        q_out = _empty(new_q, q.dtype, q.device, stream)
     po = _p(q_out)
     if po is not None:
         for name, t, n in (("q", q, ext[0]), ("k", k, ext[1]), ("v", v, ext[2])):
@@ -338,7 +346,8 @@ def _plan_store(pool, cache, table, lens):
 
 
 class PagedDecoder:
-    """Holds the workspace and the output rows for attention over pages with a fixed number of rows and blocks."""
+    """Holds the workspace and the output rows for attention over pages with a fixed number of rows and blocks.  Calls, and
+    graphs that captured them, share both: on several streams at once use a decoder for each."""
 
     def __init__(self, pool: PagePool, n_rows: int, n_q_heads: int, max_blocks: int, dtype=None, softmax_scale: float = 0.0):
         self.pool, self.n_rows, self.n_q_heads, self.max_blocks = pool, n_rows, n_q_heads, max_blocks
@@ -363,15 +372,16 @@ class PagedDecoder:
             if len(self._calls) >= 64:
                 self._calls.clear()
             call = self._calls[key] = self._plan(q, table, lens, out)
-        if out is not self.out:
+        params, q_bytes, out_bytes = call
+        pool, pq, po = self.pool, q.data_ptr(), out.data_ptr()
+        if pq < po + out_bytes and po < pq + q_bytes:
             _want_no_overlap("out", out, "q", q, False)
-        pool = self.pool
-        _call(load_library().meda_paged_attention, pool.index, stream, pool.ref, call, q.data_ptr(), table.data_ptr(), lens.data_ptr(),
-              out.data_ptr(), self.workspace.data_ptr(), self._workspace_bytes)
+        _call(load_library().meda_paged_attention, pool.index, stream, pool.ref, params, pq, table.data_ptr(), lens.data_ptr(), po,
+              self.workspace.data_ptr(), self._workspace_bytes)
         return out
 
     def _plan(self, q, table, lens, out):
-        """The checks of a call and its parameters."""
+        """The checks of a call, its parameters, and the extents of q and out."""
         pool, shape = self.pool, (self.n_rows, self.n_q_heads, self.pool.head_dim)
         for name, t in (("q", q), ("out", out)):
             _want_rows(name, t, shape, self.dtype, pool.device)
@@ -383,8 +393,9 @@ class PagedDecoder:
         if R != self.n_rows or blocks != self.max_blocks:
             raise ValueError(f"table: expected {self.n_rows} rows of {self.max_blocks} blocks")
         p, row = self.params, shape[1] * shape[2]
-        return ctypes.byref(MedaPagedParams(q.stride(0) if R > 1 else row, out.stride(0) if R > 1 else row, ts, ls, R, shape[1],
-                                            blocks, p.dtype, p.softmax_scale))
+        params = MedaPagedParams(q.stride(0) if R > 1 else row, out.stride(0) if R > 1 else row, ts, ls, R, shape[1], blocks, p.dtype,
+                                 p.softmax_scale)
+        return ctypes.byref(params), _extent(q, (0, 1, 2)), _extent(out, (0, 1, 2))
 
 
 def meda_page_update_workspace_bytes(n_rows: int) -> int:
@@ -408,7 +419,7 @@ def meda_page_update(lens: torch.Tensor, n_new: torch.Tensor, table: torch.Tenso
                                            workspace))
     params, dev, max_new, need = plan
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=table.device)
+        workspace = _empty(need, torch.uint8, table.device, stream)
     _call(load_library().meda_page_update, dev, stream, params, lens.data_ptr(), n_new.data_ptr(), table.data_ptr(), free_ring.data_ptr(),
           free_state.data_ptr(), lens_out.data_ptr(), free_state_out.data_ptr(), slots.data_ptr() if max_new else None, _p(granted),
           workspace.data_ptr(), workspace.shape[0])
@@ -462,8 +473,9 @@ class PagedCache:
 
     Row ``s * n_layers + l`` of ``table``, ``lens``, ``slots`` and ``granted`` belongs to layer l of sequence s.  No call
     synchronises, so the loop's body can be captured into a graph.  ``granted`` says after ``admit`` and ``step`` what each
-    row got: fewer positions than asked for where the pages did not suffice (such a row was left as it was; release the
-    sequence, or wait until others have ended).  Calls share the workspaces: use one stream, or order the streams."""
+    row got: fewer positions than asked for where the pages did not suffice.  Such a row was left as it was while other
+    layers of its sequence may have grown: release the sequence.  Calls share the workspaces: use one stream, or order the
+    streams."""
 
     def __init__(self, n_seqs: int, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, max_len: int, n_pages: int,
                  page_size: int = 64, dtype=torch.bfloat16, rope: Optional[RotaryPlan] = None, softmax_scale: float = 0.0,
@@ -495,12 +507,14 @@ class PagedCache:
         n, layers = layer_len.shape
         if layers != self.n_layers or first < 0 or first + n > self.n_seqs:
             raise ValueError(f"expected {self.n_layers} layers and sequences below {self.n_seqs}")
+        rows = slice(first * layers, (first + n) * layers)
+        table, lens = self.table[rows], self.lens[rows]
+        _plan_store(self.pool, cache, table, lens)      # (a cache that does not fit is refused before anything changes)
         self.release(range(first, first + n))
         self._new.zero_()
         self._new[first:first + n].copy_(layer_len)
         self._update()
-        rows = slice(first * layers, (first + n) * layers)
-        meda_paged_store(self.pool, cache, self.table[rows], self.lens[rows])
+        meda_paged_store(self.pool, cache, table, lens)
         return self.granted.view(self.n_seqs, layers)[first:first + n]
 
     def step(self, active: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -523,9 +537,9 @@ class PagedCache:
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
                positions: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
-        """k, v [n_seqs][Hkv][d] of the step's tokens enter the layer; returns q [n_seqs][Hq][d], rotated."""
-        rope = self.rope if positions is not None else None
-        return meda_paged_append(self.pool, k, v, self._rows(layer)[2], q, positions, rope, q_out)
+        """k, v [n_seqs][Hkv][d] of the step's tokens enter the layer; returns q [n_seqs][Hq][d].  k and q are rotated by
+        ``positions`` where the cache has a plan of the rotation; without one they are taken as they are."""
+        return meda_paged_append(self.pool, k, v, self._rows(layer)[2], q, positions, self.rope, q_out)
 
     def attend(self, layer: int, q: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of q [n_seqs][Hq][d] over the layer's positions, the step's own included (without ``out`` the result

@@ -217,3 +217,98 @@ def test_refusals():
     three = pkg.PagedCache(2, L + 1, Hq, Hkv, d, max_len=T, n_pages=40, page_size=16, dtype=torch.float32)
     with pytest.raises(ValueError):
         three.admit(0, compressed)
+
+
+def _state(cache):
+    return [getattr(cache, name).clone() for name in ("lens", "table", "free_ring", "free_state")] + [cache.pool.k_pages.clone()]
+
+
+def test_a_cache_that_does_not_fit_is_refused_before_anything_changes():
+    import dataclasses
+    import paper_2502_17599_amd as pkg
+    L, Hq, Hkv, d = 2, 4, 2, 64
+    rope, compressed, T = _prompts(1, L, Hq, Hkv, d, "f32", 0, 32, 2 * 100, 95)
+    cache = pkg.PagedCache(1, L, Hq, Hkv, d, max_len=T, n_pages=40, page_size=16, dtype=torch.float32, rope=rope)
+    cache.pool.k_pages.zero_()
+    cache.admit(0, compressed)
+    before = _state(cache)
+    half = dataclasses.replace(compressed, k_out=compressed.k_out.to(torch.bfloat16))
+    heads = dataclasses.replace(compressed, n_kv_heads=Hkv + 1)
+    x = normal(1, 1, Hkv, d)
+    for call in (lambda: cache.admit(0, half), lambda: cache.admit(0, heads),
+                 lambda: cache.append(0, x, x),                         # the cache rotates: by which positions?
+                 lambda: cache.append(0, x, x, normal(2, 1, Hq, d))):
+        with pytest.raises(ValueError):
+            call()
+    assert all(torch.equal(a, b) for a, b in zip(before, _state(cache)))
+
+
+def test_output_over_queries_is_refused():
+    """The decoder's own output as the next call's queries, as they lie and one row further."""
+    import paper_2502_17599_amd as pkg
+    R, Hq, Hkv, d = 3, 4, 2, 64
+    pool = pkg.PagePool.empty(4, Hkv, 16, d, torch.float32)
+    table = torch.zeros((R, 1), dtype=torch.int32, device=DEV)
+    lens = torch.zeros(R, dtype=torch.int32, device=DEV)
+    dec = pkg.PagedDecoder(pool, R, Hq, 1)
+    two = torch.zeros((R + 1, Hq, d), dtype=torch.float32, device=DEV)
+    with pytest.raises(ValueError):
+        dec(dec(two[:R], table, lens), table, lens)
+    with pytest.raises(ValueError):
+        dec(two[1:], table, lens, two[:R])
+    assert (dec(two[:R], table, lens, torch.ones_like(two[:R])) == 0).all()
+
+
+def _stream_of(t):
+    """The stream whose memory holds a tensor."""
+    for s in torch.cuda.memory_snapshot():
+        if s["address"] <= t.data_ptr() < s["address"] + s["total_size"]:
+            return s["stream"]
+
+
+def test_outputs_made_for_a_stream_come_from_its_memory():
+    """Memory of the current stream could still be in use there when a call on another stream writes to it."""
+    import paper_2502_17599_amd as pkg
+    T, H, d = 33, 2, 64
+    side = torch.cuda.Stream()
+    rope = pkg.RotaryPlan(torch.ones(d // 2, dtype=torch.float64, device=DEV))
+    x, pos = normal(1, T, H, d), torch.arange(T, dtype=torch.int32, device=DEV)
+    pool = pkg.PagePool.empty(4, H, 16, d, torch.float32)
+    want = pkg.meda_rotary(x, x, pos, rope)[0]
+    side.wait_stream(torch.cuda.current_stream())
+    q, k = pkg.meda_rotary(x, x, pos, rope, stream=side)
+    a = pkg.meda_paged_append(pool, x, x, torch.arange(T, device=DEV), x, pos, rope, stream=side)
+    torch.cuda.synchronize()
+    for t in (q, k, a):
+        assert _stream_of(t) == side.cuda_stream and torch.equal(t, want)
+
+
+def test_two_streams_at_once():
+    """Two caches, each on a stream of its own and nothing between them, against the same work one after the other."""
+    import paper_2502_17599_amd as pkg
+    L, Hq, Hkv, d, N, steps = 2, 8, 2, 64, 40, 12
+    x = [normal(200 + i, N, Hq + 2 * Hkv, d, dtype="bf16") for i in range(2)]
+
+    def make():
+        cache = pkg.PagedCache(N, L, Hq, Hkv, d, max_len=4000, n_pages=N * L * 3, page_size=16)
+        return cache, torch.zeros((steps, L, N, Hq, d), dtype=torch.bfloat16, device=DEV)
+
+    def work(cache, outs, y):
+        for s in range(steps):
+            cache.step()
+            for l in range(L):
+                cache.append(l, y[:, Hq:Hq + Hkv], y[:, Hq + Hkv:])
+                cache.attend(l, y[:, :Hq], outs[s, l])
+
+    alone, together = [make() for _ in range(2)], [make() for _ in range(2)]
+    for i in range(2):
+        work(*alone[i], x[i])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for i in range(2):
+        with torch.cuda.stream(streams[i]):
+            work(*together[i], x[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert torch.equal(alone[i][1], together[i][1])
+        assert torch.equal(alone[i][0].lens, together[i][0].lens) and torch.equal(alone[i][0].table, together[i][0].table)
