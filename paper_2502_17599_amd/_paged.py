@@ -40,7 +40,9 @@ def _empty(shape, dtype, device, stream):
 
 
 # A call of a kind that was checked before (the same shapes, strides, types and devices) is not checked again: half of the
-# time of a small call went into it.  What an entry holds depends on nothing else, addresses least of all.
+# time of a small call went into it.  What an entry holds depends on nothing else, addresses least of all.  (Keys of the
+# calls of every layer are spelled out: with a function per tensor an append of 64 tokens took 7.4 us instead of 7.1, a step of
+# attention 8.6 instead of 7.9 on the host.)
 _checked: dict = {}
 
 
@@ -186,7 +188,11 @@ def meda_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Ten
     """Rotary positions of q [T][Hq][d] and k [T][Hk][d] (any strides with contiguous rows; ``x.transpose(0, 1)`` of an
     [H][T][d] array is such a view).  The outputs may be the inputs; without them new ones are made.  ``inverse`` turns
     back: the gradient of the rotation."""
-    key = ("rotary", _kind(q), _kind(k), _kind(positions), None if rope is None else rope.key, _kind(q_out), _kind(k_out), inverse)
+    key = ("rotary", None if rope is None else rope.key, inverse, q.shape, q.stride(), q.dtype, q.get_device(),
+           positions if positions is None else (positions.shape, positions.stride(), positions.dtype, positions.get_device()),
+           k if k is None else (k.shape, k.stride(), k.dtype, k.get_device()),
+           q_out if q_out is None else (q_out.shape, q_out.stride(), q_out.dtype, q_out.get_device()),
+           k_out if k_out is None else (k_out.shape, k_out.stride(), k_out.dtype, k_out.get_device()))
     plan = _checked.get(key)
     if plan is None:
         plan = _remember(key, _plan_rotary(q, k, positions, rope, q_out, k_out, inverse))
@@ -246,7 +252,11 @@ def meda_paged_append(pool: PagePool, k: torch.Tensor, v: torch.Tensor, slots: t
                       stream=None) -> Optional[torch.Tensor]:
     """Writes k, v [M][Hkv][d] of new tokens to their ``slots`` (int64 [M], -1: none), k rotated where a plan is given;
     returns q [M][Hq][d] rotated alike (``q_out``, which may be q)."""
-    key = ("append", pool.key, _kind(k), _kind(v), _kind(slots), _kind(q), _kind(positions), None if rope is None else rope.key, _kind(q_out))
+    key = ("append", pool.key, None if rope is None else rope.key, k.shape, k.stride(), k.dtype, k.get_device(),
+           v.shape, v.stride(), v.dtype, v.get_device(), slots.shape, slots.stride(), slots.dtype, slots.get_device(),
+           q if q is None else (q.shape, q.stride(), q.dtype, q.get_device()),
+           positions if positions is None else (positions.shape, positions.stride(), positions.dtype, positions.get_device()),
+           q_out if q_out is None else (q_out.shape, q_out.stride(), q_out.dtype, q_out.get_device()))
     plan = _checked.get(key)
     if plan is None:
         plan = _remember(key, _plan_append(pool, k, v, slots, q, positions, rope, q_out))
@@ -366,7 +376,8 @@ class PagedDecoder:
         """q [rows][Hq][d] (rows any distance apart) over the pages of ``table`` [rows][blocks]; ``lens`` [rows].  Without
         ``out`` the result lies in a buffer that the next call overwrites."""
         out = self.out if out is None else out
-        key = (_kind(q), _kind(table), _kind(lens), _kind(out))
+        key = (q.shape, q.stride(), q.dtype, q.get_device(), table.shape, table.stride(), table.dtype, table.get_device(),
+               lens.shape, lens.stride(), lens.dtype, lens.get_device(), out.shape, out.stride(), out.dtype, out.get_device())
         call = self._calls.get(key)
         if call is None:
             if len(self._calls) >= 64:
