@@ -113,10 +113,11 @@ __global__ void __launch_bounds__(kLocateThreads) paged_store_kernel(StoreArgs a
 
 template <typename T, int D, bool CODES>
 static hipError_t launch_store(const StoreArgs& a, hipStream_t s) {
-  // A workgroup for every four pieces that the source rows make, a piece per wave.  (Few workgroups that walk over many pieces
-  // wait for page numbers and offsets in every step: 57 MB of 32 short layers 23 us with 16 pieces per workgroup, 13.6 with
-  // four; 596 MB 124 and 111, 1968 MB to 8 bits 399 with at most 4096 workgroups and 362 with all of them.)
-  long long groups = (a.n_src_rows / kPiece + 3) / 4 + 1;
+  // A workgroup for every four pieces that the source rows can make, whole ones and a last one of every (row, head): a piece per
+  // wave.  (Few workgroups that walk over many pieces wait for page numbers and offsets in every step: 57 MB of 32 short layers
+  // 23 us with 16 pieces per workgroup, 13.6 with four; 596 MB 124 and 111, 1968 MB to 8 bits 399 with at most 4096 workgroups
+  // and 362 with all of them.  90 layers of one or two positions in 16 heads 25 us without the last pieces counted, 9 with them.)
+  long long groups = (a.n_src_rows / kPiece + (long long)a.R * a.pool.Hkv + 3) / 4;
   if (groups > 1 << 22) groups = 1 << 22;   // (every workgroup then takes several)
   hipLaunchKernelGGL((paged_store_kernel<T, D, CODES>), dim3((unsigned)groups), dim3(kLocateThreads), 0, s, a);
   return hipGetLastError();
