@@ -20,7 +20,7 @@ namespace meda {
 
 constexpr int kAttThreads = kLocateThreads, kAttWaves = kAttThreads / 64;
 constexpr int kBlock = 16;        // positions of one matrix instruction; they lie in one page
-constexpr int kMinUnits = 4;      // a workgroup's share, at least: a step per wave
+constexpr int kMinUnits = 4;      // a workgroup's share, at least: a step per wave (kFineShares: or two)
 constexpr int kMaxGroup = 16;     // query heads per kv head
 // positions of a unit, a step of one wave: two blocks, of 4-byte rows one (as many bytes)
 constexpr int unit_positions(int bytes) { return bytes == 4 ? kBlock : 2 * kBlock; }
@@ -33,11 +33,12 @@ struct PagedArgs {
   const int32_t* lens;
   float* part;             // [2 * groups][G][d]: value sums of the pieces
   float2* part_mz;         // [2 * groups][G]: their maximum (unscaled logits) and normaliser
-  int2* cut;               // [groups]: the (row, kv head) that begins in the share and goes on behind it, as
-                           // (row * Hkv + head, shares it reaches into); (0, 0): none
+  int2* cut;               // which (row, kv head) is cut: see below
   long long q_stride, out_stride;   // bytes
   long long table_stride, len_stride;
   int R, Hq, Hkv, G, max_blocks;
+  int cut_by_pair;
+  unsigned fine_shares;    // up to so many shares may be of kMinUnits units
   float scale_log2;
 };
 
@@ -390,6 +391,12 @@ struct Attend {
 // one that goes on from the wave before (slot 0) and one that begins in it and goes on (slot 1).  After one barrier the
 // workgroup adds up the pieces of every pair, and writes it out, or, where the pair goes on in other shares, as a piece of
 // the share: slot 0 and 1 again, in memory, for the join.
+//
+// What the join finds: where there are no more pairs than workgroups, for every pair (the share that it begins in, shares
+// behind that it reaches into), and for every share the pair that begins in it and goes on behind it (row * Hkv + head,
+// shares behind) otherwise; (.., 0): nothing to join.  The join then has a workgroup for the smaller number of the two: those
+// that find nothing cost more than the others' work (32 pairs in 440 shares, eight query heads: 16.9 us with a workgroup
+// for every share, 15.1 with one for every pair; 6 pairs of long fp32 requests 40.5 and 39.5; 272 pairs 21.5 and 20.3).
 struct WavePiece {
   int pair;     // row * Hkv + head
   int shares;   // slot 1: shares behind this one that the pair reaches into
@@ -403,6 +410,10 @@ struct WavePiece {
 // cost more than the evener end gained.  Rows of 64 elements, four per CU: three fp32 requests 41.6 us, three per CU 40.1.)
 constexpr int groups_per_cu(int d, int gp) { return d == 128 && gp == 16 ? 2 : 3; }
 constexpr int kCus = 256;
+// Few pairs are cut into many pieces: past this number of shares a wave takes two steps rather than one or two, as the others
+// would wait for it, and the join has fewer pieces to read (one request of 30000 positions, 4 heads: 768 shares 24.9 us, 469
+// 21.7).  Many pairs are cut into few pieces anyhow (272 pairs of 26 to 871 fp32 positions: 768 shares 19.9 us, 540 20.9).
+constexpr int kFineShares = 2 * kCus, kFewPairs = 64;
 
 template <typename T>
 __device__ __forceinline__ void write_out(const PagedArgs& a, int pair, int h, int column, int D, float o, float z) {
@@ -426,7 +437,8 @@ __global__ void __launch_bounds__(kAttThreads, (groups_per_cu(D, GP))) paged_att
   const RowOfUnit at = locate_row(
       a.R, a.Hkv, units,
       [&](unsigned total) {
-        const unsigned shares = min((total + kMinUnits - 1) / kMinUnits, gridDim.x);
+        const unsigned fine = min((total + kMinUnits - 1) / kMinUnits, a.fine_shares);
+        const unsigned shares = min(max(fine, (total + 2 * kMinUnits - 1) / (2 * kMinUnits)), gridDim.x);
         if (id >= (int)shares) return;
         cut_in = Shares(total, shares);
         share = cut_in.first(id);
@@ -457,6 +469,7 @@ __global__ void __launch_bounds__(kAttThreads, (groups_per_cu(D, GP))) paged_att
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        if (a.cut_by_pair && (threadIdx.x & 63) == 0) a.cut[pair] = make_int2(0, 0);
       } else if ((threadIdx.x & 63) == 0) {
         pieces[wave][slot] = WavePiece{pair, (int)cut_in.share_of(beg + (n - u - take) - 1) - id, true, u + take == n};
       }
@@ -525,16 +538,23 @@ __global__ void __launch_bounds__(kAttThreads, (groups_per_cu(D, GP))) paged_att
       }
     }
     if (slot == 1) {
-      if (!ends) cut = make_int2(first.pair, first.shares);
+      if (a.cut_by_pair) {
+        if (threadIdx.x == 0) a.cut[first.pair] = make_int2(id, ends ? 0 : first.shares);
+      } else if (!ends) {
+        cut = make_int2(first.pair, first.shares);
+      }
       todo &= todo - 1u;
     }
     slot = 1;
   }
-  if (threadIdx.x == 0) a.cut[id] = cut;
+  if (!a.cut_by_pair && threadIdx.x == 0) a.cut[id] = cut;
   // rows without positions, dealt to all workgroups
   for (int r = id; r < a.R; r += gridDim.x)
-    if (row_len(a, r) == 0)
+    if (row_len(a, r) == 0) {
       for (int i = threadIdx.x; i < a.Hq * D; i += kAttThreads) store_elem(a.out + r * a.out_stride + (size_t)i * sizeof(T), 0.f, T{});
+      if (a.cut_by_pair)
+        for (int i = threadIdx.x; i < a.Hkv; i += kAttThreads) a.cut[r * a.Hkv + i] = make_int2(0, 0);
+    }
 }
 
 // ---- short tables -----------------------------------------------------------------------------------------------------
@@ -548,7 +568,7 @@ __global__ void __launch_bounds__(kAttThreads, (groups_per_cu(D, GP))) paged_att
 // 6.9 and 9.9; beyond: 128 pairs of up to 1023 20 and 18, 8 pairs of 1023 15 and 10, 8 pairs of 1000 8-bit positions 14 and
 // 11).  Eight waves where every workgroup has a CU to itself, four otherwise (128 pairs of up to 600 13.6 and 14.2 us with
 // eight and four, 2000 pairs of up to 300 51 and 30).
-constexpr int kPairBytes = 320 << 10, kPairPositions = 512, kFewPairs = 64;
+constexpr int kPairBytes = 320 << 10, kPairPositions = 512;
 template <typename T, int D, int GP, bool FP8, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, (WAVES == 4 ? groups_per_cu(D, GP) : 2)) paged_pair_kernel(PagedArgs a) {
   using At = Attend<T, D, GP, FP8>;
@@ -580,20 +600,20 @@ __global__ void __launch_bounds__(64 * WAVES, (WAVES == 4 ? groups_per_cu(D, GP)
   }
 }
 
-// grid (workgroups of the first kernel, G), 256 threads: joins the pieces of the (row, kv head) that share blockIdx.x cuts, one
-// query head each.  Four columns per thread, kLanes pieces side by side and eight of each on their way together: a request
-// cut into 128 pieces takes two rounds, one of 64 columns per row one.  768 shares of seven heads, most of them cut in two or
-// three: 4.3 us; three long fp32 requests cut into 128 pieces per head: 6.3 us with eight pieces side by side (half as many:
-// 9.5 us; one column per thread, two pieces side by side: 10).
-constexpr int kJoinThreads = 256;
-template <typename T, int D>
+// grid (pairs or shares, G): joins the pieces of the (row, kv head) that blockIdx.x names, one query head each.  Four columns per
+// thread, kJoinLanes pieces side by side and eight of each on their way together: 128 pieces take two rounds, or one with 64
+// columns per row.  (256 pairs of seven heads, most of them cut in two or three: 4.6 us, 6.0 with 512 threads; four pairs cut
+// into 192 pieces 6.0 and 5.4.  One column per thread, two pieces side by side: twice as long.)
+constexpr int kJoinPieces = 128;
+template <typename T, int D, int kJoinThreads>
 __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a) {
   constexpr int Q = D / 4, kJoinLanes = kJoinThreads / Q, U = 8;
   __shared__ float4 lds_o[kJoinLanes][Q];
   __shared__ float lds_m[kJoinLanes], lds_z[kJoinLanes];
-  const int id = blockIdx.x, h = blockIdx.y, j = threadIdx.x % Q, lane = threadIdx.x / Q;
-  const int2 cut = a.cut[id];
+  const int h = blockIdx.y, j = threadIdx.x % Q, lane = threadIdx.x / Q;
+  const int2 cut = a.cut[blockIdx.x];
   if (cut.y == 0) return;
+  const int id = a.cut_by_pair ? cut.x : (int)blockIdx.x, pair = a.cut_by_pair ? (int)blockIdx.x : cut.x;
   const int n = cut.y + 1;   // pieces: slot 1 of share id, slot 0 of the shares behind it
   float mn = kLeast, zs = 0.f;
   float4 os = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -650,7 +670,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a) {
     zs = fmaf(lds_z[w], c, zs);
     add(os, lds_o[w][j], c);
   }
-  const int r = cut.x / a.Hkv, head = cut.x - r * a.Hkv;
+  const int r = pair / a.Hkv, head = pair - r * a.Hkv;
   char* dst = a.out + r * a.out_stride + ((size_t)(head * a.G + h) * D + 4 * j) * sizeof(T);
   const float x[4] = {os.x, os.y, os.z, os.w};
 #pragma unroll
@@ -712,7 +732,9 @@ static hipError_t launch_paged(const PagedPlan& pl, const PagedArgs& a, hipStrea
   hipLaunchKernelGGL((paged_attention_kernel<T, D, GP, FP8>), dim3(pl.groups), dim3(kAttThreads), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(pl.groups, a.G), dim3(kJoinThreads), 0, s, a);
+  const int joins = a.cut_by_pair ? a.R * a.Hkv : pl.groups;
+  if (pl.groups >= kJoinPieces * joins) hipLaunchKernelGGL((paged_join_kernel<T, D, 512>), dim3(joins, a.G), dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((paged_join_kernel<T, D, 256>), dim3(joins, a.G), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 template <typename T, int D, bool FP8>
@@ -761,6 +783,9 @@ meda_status meda_paged_attention(const meda_page_pool* pool, const meda_paged_pa
   a.table_stride = p.table_stride ? p.table_stride : p.max_blocks;
   a.len_stride = p.len_stride ? p.len_stride : 1;
   a.R = p.n_rows; a.Hq = p.n_q_heads; a.Hkv = pool->n_kv_heads; a.G = a.Hq / a.Hkv; a.max_blocks = p.max_blocks;
+  const int64_t pairs = (int64_t)p.n_rows * pool->n_kv_heads;
+  a.cut_by_pair = pairs <= pl.groups;
+  a.fine_shares = pairs <= kFewPairs ? kFineShares : pl.groups;
   const double scale = p.softmax_scale > 0.0f ? (double)p.softmax_scale : 1.0 / sqrt((double)pool->head_dim);
   a.scale_log2 = (float)(scale * 1.4426950408889634074);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
