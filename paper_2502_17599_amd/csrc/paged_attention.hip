@@ -415,18 +415,33 @@ constexpr int kCus = 256;
 // 21.7).  Many pairs are cut into few pieces anyhow (272 pairs of 26 to 871 fp32 positions: 768 shares 19.9 us, 540 20.9).
 constexpr int kFineShares = 2 * kCus, kFewPairs = 64;
 
+// Four columns of a row of out; a sum of weights of zero (every page is missing) gives zeros.
+__device__ __forceinline__ void store4(char* dst, const float (&x)[4], float) {
+  *reinterpret_cast<float4*>(dst) = make_float4(x[0], x[1], x[2], x[3]);
+}
+__device__ __forceinline__ void store4(char* dst, const float (&x)[4], bf16_t) {
+  *reinterpret_cast<uint2*>(dst) = make_uint2(float_to_bf16_rne(x[0]) | (float_to_bf16_rne(x[1]) << 16),
+                                              float_to_bf16_rne(x[2]) | (float_to_bf16_rne(x[3]) << 16));
+}
 template <typename T>
-__device__ __forceinline__ void write_out(const PagedArgs& a, int pair, int h, int column, int D, float o, float z) {
+__device__ __forceinline__ void write_out(const PagedArgs& a, int pair, int h, int column, int D, const float4& o, float z) {
   const int r = pair / a.Hkv, head = pair - r * a.Hkv;
-  // (no weight at all, as where every page is missing: zeros)
-  store_elem(a.out + r * a.out_stride + ((size_t)(head * a.G + h) * D + column) * sizeof(T), z == 0.f ? 0.f : o / z, T{});
+  const float x[4] = {z == 0.f ? 0.f : o.x / z, z == 0.f ? 0.f : o.y / z, z == 0.f ? 0.f : o.z / z, z == 0.f ? 0.f : o.w / z};
+  store4(a.out + r * a.out_stride + ((size_t)(head * a.G + h) * D + column) * sizeof(T), x, T{});
+}
+__device__ __forceinline__ float4 scaled(const float4& x, float c) { return make_float4(x.x * c, x.y * c, x.z * c, x.w * c); }
+__device__ __forceinline__ float4 add_scaled(const float4& sum, const float4& x, float c) {
+  return make_float4(fmaf(x.x, c, sum.x), fmaf(x.y, c, sum.y), fmaf(x.z, c, sum.z), fmaf(x.w, c, sum.w));
+}
+__device__ __forceinline__ float4 either(bool first, const float4& x, const float4& y) {
+  return make_float4(first ? x.x : y.x, first ? x.y : y.y, first ? x.z : y.z, first ? x.w : y.w);
 }
 
 // grid: groups_per_cu workgroups for every CU, or fewer (a share of kMinUnits units for each of the most that there can be).
 template <typename T, int D, int GP, bool FP8>
 __global__ void __launch_bounds__(kAttThreads, (groups_per_cu(D, GP))) paged_attention_kernel(PagedArgs a) {
   using At = Attend<T, D, GP, FP8>;
-  __shared__ float red_o[kAttWaves][2][GP][D];
+  __shared__ __align__(16) float red_o[kAttWaves][2][GP][D];
   __shared__ float red_m[kAttWaves][2][GP], red_z[kAttWaves][2][GP];
   __shared__ WavePiece pieces[kAttWaves][2];
   const int id = blockIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -464,8 +479,10 @@ __global__ void __launch_bounds__(kAttThreads, (groups_per_cu(D, GP))) paged_att
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        for (int i = threadIdx.x & 63; i < a.G * D; i += 64)
-          write_out<T>(a, pair, i / D, i % D, D, red_o[wave][1][i / D][i % D], red_z[wave][1][i / D]);
+        for (int i = threadIdx.x & 63; i < a.G * (D / 4); i += 64) {
+          const int h = i / (D / 4), j = 4 * (i - h * (D / 4));
+          write_out<T>(a, pair, h, j, D, *reinterpret_cast<const float4*>(&red_o[wave][1][h][j]), red_z[wave][1][h]);
+        }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -511,8 +528,8 @@ __global__ void __launch_bounds__(kAttThreads, (groups_per_cu(D, GP))) paged_att
       more &= (2u << __builtin_ctz(last)) - 1u;
     }
     const WavePiece first = pieces[w0][slot];
-    for (int i = threadIdx.x; i < a.G * D; i += kAttThreads) {
-      const int h = i / D, j = i - h * D;
+    for (int i = threadIdx.x; i < a.G * (D / 4); i += kAttThreads) {   // (four columns: one round for groups of up to 8 heads)
+      const int h = i / (D / 4), j = 4 * (i - h * (D / 4));
       float m[kAttWaves], mn = red_m[w0][slot][h];
       const float m0 = mn;
 #pragma unroll
@@ -521,19 +538,20 @@ __global__ void __launch_bounds__(kAttThreads, (groups_per_cu(D, GP))) paged_att
         mn = (more >> w) & 1u ? fmaxf(mn, m[w]) : mn;
       }
       float c = weight_under(m0, mn, a.scale_log2);
-      float zs = red_z[w0][slot][h] * c, os = red_o[w0][slot][h][j] * c;
+      float zs = red_z[w0][slot][h] * c;
+      float4 os = scaled(*reinterpret_cast<const float4*>(&red_o[w0][slot][h][j]), c);
 #pragma unroll
       for (int w = 1; w < kAttWaves; ++w) {
         c = weight_under(m[w], mn, a.scale_log2);
-        const float z = fmaf(red_z[w][0][h], c, zs), o = fmaf(red_o[w][0][h][j], c, os);
-        zs = (more >> w) & 1u ? z : zs;
-        os = (more >> w) & 1u ? o : os;
+        const bool in = ((more >> w) & 1u) != 0u;
+        zs = in ? fmaf(red_z[w][0][h], c, zs) : zs;
+        os = either(in, add_scaled(os, *reinterpret_cast<const float4*>(&red_o[w][0][h][j]), c), os);
       }
       if (slot == 1 && ends) {
         write_out<T>(a, first.pair, h, j, D, os, zs);
       } else {
         const size_t to = (size_t)(2 * id + slot) * a.G + h;
-        a.part[to * D + j] = os;
+        *reinterpret_cast<float4*>(a.part + to * D + j) = os;
         if (j == 0) a.part_mz[to] = make_float2(mn, zs);
       }
     }
@@ -572,7 +590,7 @@ constexpr int kPairBytes = 320 << 10, kPairPositions = 512;
 template <typename T, int D, int GP, bool FP8, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, (WAVES == 4 ? groups_per_cu(D, GP) : 2)) paged_pair_kernel(PagedArgs a) {
   using At = Attend<T, D, GP, FP8>;
-  __shared__ float red_o[WAVES][GP][D];
+  __shared__ __align__(16) float red_o[WAVES][GP][D];
   __shared__ float red_m[WAVES][GP], red_z[WAVES][GP];
   const int head = blockIdx.x, r = blockIdx.y, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int len = __builtin_amdgcn_readfirstlane(row_len(a, r)), n = (len + At::kUnit - 1) / At::kUnit;
@@ -584,17 +602,17 @@ __global__ void __launch_bounds__(64 * WAVES, (WAVES == 4 ? groups_per_cu(D, GP)
     st.put(red_o[wave], red_m[wave], red_z[wave]);
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < a.G * D; i += 64 * WAVES) {
-    const int h = i / D, j = i - h * D;
-    float mn = kLeast, zs = 0.f, os = 0.f;
+  for (int i = threadIdx.x; i < a.G * (D / 4); i += 64 * WAVES) {
+    const int h = i / (D / 4), j = 4 * (i - h * (D / 4));
+    float mn = kLeast, zs = 0.f;
+    float4 os = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) mn = w < active ? fmaxf(mn, red_m[w][h]) : mn;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
       const float c = weight_under(red_m[w][h], mn, a.scale_log2);
-      const float z = fmaf(red_z[w][h], c, zs), o = fmaf(red_o[w][h][j], c, os);
-      zs = w < active ? z : zs;
-      os = w < active ? o : os;
+      zs = w < active ? fmaf(red_z[w][h], c, zs) : zs;
+      os = either(w < active, add_scaled(os, *reinterpret_cast<const float4*>(&red_o[w][h][j]), c), os);
     }
     write_out<T>(a, r * a.Hkv + head, h, j, D, os, zs);
   }
@@ -617,9 +635,6 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a) {
   const int n = cut.y + 1;   // pieces: slot 1 of share id, slot 0 of the shares behind it
   float mn = kLeast, zs = 0.f;
   float4 os = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto add = [](float4& acc, const float4& x, float c) {
-    acc.x = fmaf(x.x, c, acc.x); acc.y = fmaf(x.y, c, acc.y); acc.z = fmaf(x.z, c, acc.z); acc.w = fmaf(x.w, c, acc.w);
-  };
   auto round = [&](int s0, auto count) {
     constexpr int N = decltype(count)::value;
     float2 mz[N];
@@ -639,13 +654,13 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a) {
     for (int u = 0; u < N; ++u) top = fmaxf(top, mz[u].x);   // (a piece that is repeated changes no maximum)
     const float c0 = weight_under(mn, top, a.scale_log2);
     zs *= c0;
-    os.x *= c0; os.y *= c0; os.z *= c0; os.w *= c0;
+    os = scaled(os, c0);
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const bool in = s0 + u * kJoinLanes < n;
       const float c = in ? weight_under(mz[u].x, top, a.scale_log2) : 0.f;
       zs = fmaf(in ? mz[u].y : 0.f, c, zs);
-      add(os, make_float4(in ? o[u].x : 0.f, in ? o[u].y : 0.f, in ? o[u].z : 0.f, in ? o[u].w : 0.f), c);
+      os = add_scaled(os, either(in, o[u], make_float4(0.f, 0.f, 0.f, 0.f)), c);
     }
     mn = top;
   };
@@ -668,13 +683,9 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a) {
   for (int w = 0; w < kJoinLanes; ++w) {
     const float c = weight_under(lds_m[w], mn, a.scale_log2);
     zs = fmaf(lds_z[w], c, zs);
-    add(os, lds_o[w][j], c);
+    os = add_scaled(os, lds_o[w][j], c);
   }
-  const int r = pair / a.Hkv, head = pair - r * a.Hkv;
-  char* dst = a.out + r * a.out_stride + ((size_t)(head * a.G + h) * D + 4 * j) * sizeof(T);
-  const float x[4] = {os.x, os.y, os.z, os.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) store_elem(dst + i * sizeof(T), zs == 0.f ? 0.f : x[i] / zs, T{});
+  write_out<T>(a, pair, h, 4 * j, D, os, zs);
 }
 
 struct PagedPlan {
