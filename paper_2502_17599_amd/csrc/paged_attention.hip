@@ -580,13 +580,15 @@ __global__ void __launch_bounds__(kAttThreads, (groups_per_cu(D, GP))) paged_att
 // Where no row can be long, a workgroup per (row, kv head) is enough: no search, no pieces in memory, no second launch.
 // WAVES contiguous parts of the pair's units, added up in LDS.  grid (Hkv, R).
 //
-// A CU takes the rows of a pair in at some 150 GB/s, so a table is short up to kPairBytes of keys and values per pair, and up
-// to kPairPositions where there are too few pairs to keep the chip busy beside (pairs against shares: 2000 rows of up to 300
-// positions 30 and 39 us, 512 pairs of up to 600 23 and 28, 256 pairs of up to 1000 8-bit positions 15 and 18, 8 pairs of 100
-// 6.9 and 9.9; beyond: 128 pairs of up to 1023 20 and 18, 8 pairs of 1023 15 and 10, 8 pairs of 1000 8-bit positions 14 and
-// 11).  Eight waves where every workgroup has a CU to itself, four otherwise (128 pairs of up to 600 13.6 and 14.2 us with
-// eight and four, 2000 pairs of up to 300 51 and 30).
-constexpr int kPairBytes = 320 << 10, kPairPositions = 512;
+// How short, by the bytes of keys and values that the table can hold per pair: up to kPairBytes with enough pairs to keep the
+// chip busy (pairs against shares, us: 2000 rows of up to 300 positions 28.9 and 36.7, 512 pairs of up to 600 20.2 and 23.3,
+// 256 pairs of up to 1000 8-bit positions 14.8 and 20.3, 160 of 300 to 600 15.3 and 17.3), up to kFewPairBytes with half as many
+// pairs as CUs or fewer, where the CU with the longest row is waited for (128 pairs of up to 384 10.6 and 11.9, of up to 600 13.9
+// and 11.9; 96 of up to 300 fp32 positions 14.5 and 12.3), and with a handful up to kPairPositions, as the waves of one CU walk
+// over them (8 pairs of 100 6.1 and 8.9, of 400 9.1 and 10.3, of 1000 8-bit positions 13.9 and 10.2).  Eight waves where every
+// workgroup has a CU to itself, four otherwise (256 pairs of up to 1000 8-bit positions 14.8 and 16.9 us with eight and four,
+// 2000 pairs of up to 300 43.5 and 28.9).
+constexpr int kPairBytes = 320 << 10, kFewPairBytes = 208 << 10, kPairPositions = 512;
 template <typename T, int D, int GP, bool FP8, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, (WAVES == 4 ? groups_per_cu(D, GP) : 2)) paged_pair_kernel(PagedArgs a) {
   using At = Attend<T, D, GP, FP8>;
@@ -722,7 +724,8 @@ static meda_status make_paged_plan(const meda_page_pool* pool, const meda_paged_
   pl->groups = (int)(shares < most_groups ? shares : most_groups);
   pl->pair_waves = 0;
   const int64_t pairs = (int64_t)p->n_rows * pool->n_kv_heads;
-  if (most * 2 * pool->head_dim * dtype_bytes(pool->dtype) <= kPairBytes && (pairs > kFewPairs || most <= kPairPositions) && p->n_rows <= 65535)
+  const int64_t bytes = most * 2 * pool->head_dim * dtype_bytes(pool->dtype);
+  if (bytes <= (pairs > kCus / 2 ? kPairBytes : kFewPairBytes) && (pairs > kFewPairs || most <= kPairPositions) && p->n_rows <= 65535)
     pl->pair_waves = pairs <= kCus ? 8 : 4;
   pl->part_bytes = ((size_t)2 * pl->groups * G * pool->head_dim * sizeof(float) + 255) / 256 * 256;
   pl->mz_bytes = ((size_t)2 * pl->groups * G * sizeof(float2) + 255) / 256 * 256;

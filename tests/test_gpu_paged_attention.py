@@ -288,3 +288,29 @@ def test_long_walks_of_one_wave(cache):
     t, n = torch.from_numpy(table).to(DEV), torch.from_numpy(lens).to(DEV)
     q = normal(23, R, 2 * Hkv, 64, dtype="f32" if cache == "f32" else "bf16")
     _check(pkg.PagedDecoder(pool, R, 2 * Hkv, width)(q, t, n), q, pool, t, n, rows=(0, 3, 5, 7, 31, 40, 63))
+
+
+def test_long_rows_among_many_short_ones():
+    """More (row, kv head) pairs than workgroups, some of them cut: the join goes by shares."""
+    lens = [1 + (r * 13) % 40 for r in range(900)]
+    lens[5], lens[400], lens[899] = 9000, 33000, 5000
+    _run(lens, 4, 2, 64, "bf16", 16, seed=31, rows=[0, 4, 5, 6, 200, 399, 400, 401, 898, 899])
+
+
+@pytest.mark.parametrize("R,Hkv", [(6, 2), (450, 2)])
+def test_nothing_is_kept_from_the_call_before(R, Hkv):
+    """One decoder over long rows, short ones, none and long ones again: as a new one gives them, bit by bit."""
+    import paper_2502_17599_amd as pkg
+    page, n_pages, width = 16, 200, 1500
+    pool = make_pool("bf16", n_pages, Hkv, page, 64, seed=41)
+    rng = np.random.default_rng(42)
+    table = torch.from_numpy(rng.integers(0, n_pages, size=(R, width)).astype(np.int32)).to(DEV)
+    q = normal(43, R, 2 * Hkv, 64, dtype="bf16")
+    kept = pkg.PagedDecoder(pool, R, 2 * Hkv, width)
+    for most in (width * page, 30, 3000, 0, 500, width * page):
+        lens = torch.from_numpy(rng.integers(0, most + 1, size=R).astype(np.int32)).to(DEV)
+        if most == 3000:
+            lens[R // 2:] = 0
+        got, want = kept(q, table, lens).clone(), pkg.PagedDecoder(pool, R, 2 * Hkv, width)(q, table, lens)
+        assert torch.equal(got, want), most
+        _check(got, q, pool, table, lens, rows=(0, R // 2, R - 1))
