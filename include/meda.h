@@ -279,6 +279,9 @@ typedef struct {
  * A row is refused, its length and table unchanged, where len + m exceeds max_blocks * page_size (it then needs no pages),
  * or where it needs pages and those needed by the rows up to and including it exceed the pages that were free when the call
  * began (pages given back by the call serve the next one).
+ * With rows_per_seq = L > 1 the L rows of a sequence (its layers; rows s * L .. s * L + L - 1) are granted together: all that
+ * they ask for, or nothing where one of them exceeds its table (none of them then needs pages) or the pages needed by the rows
+ * up to and including the sequence's last exceed the free ones.  Rows that have ended give their pages back either way.
  *   lens        [R] int32; lens_out [R] int32: the new lengths (may be lens itself)
  *   table       [R][max_blocks] int32, updated in place
  *   free_ring   [n_pages] int32, updated in place: the free pages lie at head, head + 1, .. (mod n_pages); pages are taken
@@ -296,6 +299,7 @@ typedef struct {
   int32_t max_blocks;  /* columns of the table, >= 1; max_blocks * page_size < 2^31                     */
   int32_t page_size;   /* 16, 32, 64, 128 or 256                                                        */
   int32_t max_new;     /* columns of slots, >= 0                                                        */
+  int32_t rows_per_seq; /* 0 or 1: every row on its own; otherwise R is a multiple of it                */
 } meda_page_params;
 size_t meda_page_update_workspace_bytes(int32_t n_rows);
 meda_status meda_page_update(const meda_page_params* params, const int32_t* lens, const int32_t* n_new, int32_t* table,

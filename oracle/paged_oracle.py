@@ -15,8 +15,10 @@ def blocks(n: int, page: int) -> int:
     return -(-n // page)
 
 
-def page_update(lens, n_new, table, ring, state, page, max_new):
+def page_update(lens, n_new, table, ring, state, page, max_new, rows_per_seq=1):
     """Row after row, as the header describes it.  Returns (lens, table, ring, state, slots, granted), all new."""
+    if rows_per_seq > 1:
+        return _page_update_together(lens, n_new, table, ring, state, page, max_new, rows_per_seq)
     lens, table, ring = [int(x) for x in lens], np.array(table), np.array(ring)
     total, width = len(ring), table.shape[1]
     head, free = int(state[0]), int(state[1])
@@ -50,6 +52,21 @@ def page_update(lens, n_new, table, ring, state, page, max_new):
         ring[(head + free + i) % total] = x
     return (np.array(lens, np.int32), table, ring, np.array([(head + taken) % total, len(queue) + len(given)], np.int64), slots,
             np.array(granted, np.int32))
+
+
+def _page_update_together(lens, n_new, table, ring, state, page, max_new, L):
+    """The sequences that can be granted are found first; the others ask for nothing, and the rows go their way one by one."""
+    asked, wanted, refused = np.array(n_new), 0, set()
+    for s in range(0, len(lens), L):
+        rows = [r for r in range(s, s + L) if asked[r] >= 0]
+        if any(int(lens[r]) + int(asked[r]) > table.shape[1] * page for r in rows):
+            refused |= set(rows)
+            continue
+        need = sum(blocks(int(lens[r]) + int(asked[r]), page) - blocks(int(lens[r]), page) for r in rows)
+        wanted += need
+        if need and wanted > int(state[1]):
+            refused |= set(rows)
+    return page_update(lens, [0 if r in refused else m for r, m in enumerate(asked)], table, ring, state, page, max_new)
 
 
 def rotate(x, positions, inv_freq, axis=None, interleaved=False, inverse=False):

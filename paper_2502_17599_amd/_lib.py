@@ -56,7 +56,7 @@ class MedaPagePool(ctypes.Structure):
 
 class MedaPageParams(ctypes.Structure):
     _fields_ = [("n_pages", ctypes.c_int64), ("n_rows", ctypes.c_int32), ("max_blocks", ctypes.c_int32),
-                ("page_size", ctypes.c_int32), ("max_new", ctypes.c_int32)]
+                ("page_size", ctypes.c_int32), ("max_new", ctypes.c_int32), ("rows_per_seq", ctypes.c_int32)]
 
 
 class MedaRotaryParams(ctypes.Structure):

@@ -416,18 +416,20 @@ def meda_page_update_workspace_bytes(n_rows: int) -> int:
 def meda_page_update(lens: torch.Tensor, n_new: torch.Tensor, table: torch.Tensor, free_ring: torch.Tensor,
                      free_state: torch.Tensor, page_size: int, lens_out: Optional[torch.Tensor] = None,
                      free_state_out: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
-                     granted: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+                     granted: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None,
+                     rows_per_seq: int = 1) -> None:
     """Room for ``n_new`` positions per row (negative: the row has ended), from the free pages.  ``table`` [R][blocks] and
     ``free_ring`` [n_pages] are updated in place, lens [R] and free_state [2] too unless outputs for them are given;
-    ``slots`` [R][max_new] and ``granted`` [R] receive the slots and what each row got."""
+    ``slots`` [R][max_new] and ``granted`` [R] receive the slots and what each row got.  ``rows_per_seq`` consecutive rows
+    are granted together: all that they ask for, or nothing."""
     lens_out = lens if lens_out is None else lens_out
     free_state_out = free_state if free_state_out is None else free_state_out
     key = ("pages", _kind(lens), _kind(n_new), _kind(table), _kind(free_ring), _kind(free_state), page_size, _kind(lens_out),
-           _kind(free_state_out), _kind(slots), _kind(granted), _kind(workspace))
+           _kind(free_state_out), _kind(slots), _kind(granted), _kind(workspace), rows_per_seq)
     plan = _checked.get(key)
     if plan is None:
         plan = _remember(key, _plan_update(lens, n_new, table, free_ring, free_state, page_size, lens_out, free_state_out, slots, granted,
-                                           workspace))
+                                           workspace, rows_per_seq))
     params, dev, max_new, need = plan
     if workspace is None:
         workspace = _empty(need, torch.uint8, table.device, stream)
@@ -436,7 +438,7 @@ def meda_page_update(lens: torch.Tensor, n_new: torch.Tensor, table: torch.Tenso
           workspace.data_ptr(), workspace.shape[0])
 
 
-def _plan_update(lens, n_new, table, free_ring, free_state, page_size, lens_out, free_state_out, slots, granted, workspace):
+def _plan_update(lens, n_new, table, free_ring, free_state, page_size, lens_out, free_state_out, slots, granted, workspace, rows_per_seq):
     """The checks of a call, its parameters, the columns of slots, the workspace's size."""
     dev = table.device
     if not table.is_cuda:
@@ -446,6 +448,8 @@ def _plan_update(lens, n_new, table, free_ring, free_state, page_size, lens_out,
     R, blocks = table.shape
     if page_size not in PAGE_SIZES:
         raise ValueError(f"page_size {page_size}: expected one of {PAGE_SIZES}")
+    if rows_per_seq < 1 or R % rows_per_seq:
+        raise ValueError(f"rows_per_seq {rows_per_seq}: {R} rows are no multiple of it")
     for name, t, shape, dtype in (("lens", lens, (R,), torch.int32), ("n_new", n_new, (R,), torch.int32),
                                   ("table", table, (R, blocks), torch.int32), ("lens_out", lens_out, (R,), torch.int32),
                                   ("free_state", free_state, (2,), torch.int64),
@@ -465,7 +469,7 @@ def _plan_update(lens, n_new, table, free_ring, free_state, page_size, lens_out,
     if workspace is not None and (workspace.dim() != 1 or workspace.device != dev or workspace.dtype != torch.uint8
                                   or not workspace.is_contiguous()):
         raise ValueError(f"workspace: expected a contiguous uint8 vector on {dev}")
-    return (ctypes.byref(MedaPageParams(free_ring.shape[0], R, blocks, page_size, max_new)), dev.index, max_new,
+    return (ctypes.byref(MedaPageParams(free_ring.shape[0], R, blocks, page_size, max_new, rows_per_seq)), dev.index, max_new,
             meda_page_update_workspace_bytes(R))
 
 
@@ -484,9 +488,9 @@ class PagedCache:
 
     Row ``s * n_layers + l`` of ``table``, ``lens``, ``slots`` and ``granted`` belongs to layer l of sequence s.  No call
     synchronises, so the loop's body can be captured into a graph.  ``granted`` says after ``admit`` and ``step`` what each
-    row got: fewer positions than asked for where the pages did not suffice.  Such a row was left as it was while other
-    layers of its sequence may have grown: release the sequence.  Calls share the workspaces: use one stream, or order the
-    streams."""
+    row got.  Where the pages do not suffice for all layers of a sequence, none of them gets any (0) and the sequence is left
+    as it was: release others and ask again for it, or release it.  Calls share the workspaces: use one stream, or order
+    the streams."""
 
     def __init__(self, n_seqs: int, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, max_len: int, n_pages: int,
                  page_size: int = 64, dtype=torch.bfloat16, rope: Optional[RotaryPlan] = None, softmax_scale: float = 0.0,
@@ -509,7 +513,7 @@ class PagedCache:
 
     def _update(self, slots=None):
         meda_page_update(self.lens, self._new.view(-1), self.table, self.free_ring, self.free_state, self.pool.page_size,
-                         slots=slots, granted=self.granted, workspace=self._workspace)
+                         slots=slots, granted=self.granted, workspace=self._workspace, rows_per_seq=self.n_layers)
 
     def admit(self, first: int, cache: CompressedCache) -> torch.Tensor:
         """The sequences of a compressed cache become the sequences first, first + 1, ..; what these held is released.

@@ -81,7 +81,7 @@ int main() {
     if (r.n_tokens != 0) EXPECT(meda_rotary(&r, p, p, (int32_t*)p, nullptr, (uint8_t*)p, p, p, nullptr) != MEDA_OK);
     meda_page_params g;
     memset(&g, 0, sizeof g);
-    g.n_pages = pool.n_pages; g.n_rows = a.n_rows; g.max_blocks = a.max_blocks; g.page_size = pool.page_size; g.max_new = pick32(0, 100, 1);
+    g.n_pages = pool.n_pages; g.n_rows = a.n_rows; g.max_blocks = a.max_blocks; g.page_size = pool.page_size; g.max_new = pick32(0, 100, 1); g.rows_per_seq = pick32(0, 100, 1);
     EXPECT(meda_page_update(&g, nullptr, (int32_t*)p, (int32_t*)p, (int32_t*)p, (int64_t*)p, (int32_t*)p, (int64_t*)p, (int64_t*)p, nullptr, p, 1 << 24, nullptr) != MEDA_OK);
     EXPECT(meda_page_update_workspace_bytes(g.n_rows) % 256 == 0);
   }

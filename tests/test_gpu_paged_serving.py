@@ -104,31 +104,52 @@ def test_serving_loop(dtype, pages, page):
 
 
 def test_refused_rows_change_nothing():
-    """Pages for half of the prompts only: the rows of the others hold nothing and their caches are written nowhere."""
+    """Pages for one prompt and a bit: the rows of the other hold nothing and its caches are written nowhere; a step grants all
+    layers of a sequence room or none, and what was refused can be asked for again."""
     import paper_2502_17599_amd as pkg
     L, Hq, Hkv, d, N, page = 3, 4, 2, 64, 2, 16
     rope, compressed, T = _prompts(2, L, Hq, Hkv, d, "f32", 0, 32, 3 * 100, 50)
     need = ((compressed.layer_len + page - 1) // page).view(-1)
-    n_pages = int(need[:4].sum())
+    n_pages = int(need[:4].sum())                                 # those of one more layer, too few for the second prompt
     cache = pkg.PagedCache(N, L, Hq, Hkv, d, max_len=T, n_pages=n_pages, page_size=page, dtype=torch.float32)
     cache.pool.k_pages.fill_(3.0); cache.pool.v_pages.fill_(3.0)
     granted = cache.admit(0, compressed).reshape(-1)
-    assert torch.equal(granted[:4], compressed.layer_len.view(-1)[:4]) and (granted[4:] == 0).all()
-    assert torch.equal(cache.lens, granted)
+    assert torch.equal(granted[:3], compressed.layer_len.view(-1)[:3]) and (granted[3:] == 0).all()
+    assert torch.equal(cache.lens, granted) and int(cache.free_state[1]) == int(need[3])
     kp, _ = values(cache.pool)
-    k_l, _, _ = compressed.sequence(1).layer(0)
-    assert np.array_equal(P.gather(kp, cache.table[3].cpu().numpy(), int(cache.lens[3])), wide(k_l))
-    got = cache.step()
-    lens = compressed.layer_len.view(-1)[:4]
-    want = [1 if n % page else 0 for n in lens.tolist()] + [0, 0]     # room in the last page, or none
-    assert got.reshape(-1).tolist() == want
-    slots = cache.slots.view(-1).tolist()
-    assert [s >= 0 for s in slots] == [bool(w) for w in want]
-    before = cache.pool.k_pages.clone()
+    for l in range(L):
+        k_l, _, _ = compressed.sequence(0).layer(l)
+        assert np.array_equal(P.gather(kp, cache.table[l].cpu().numpy(), int(cache.lens[l])), wide(k_l))
+    held = set(cache.table[0, :int(need[0])].tolist()) | set(cache.table[1, :int(need[1])].tolist()) | set(cache.table[2, :int(need[2])].tolist())
+    free = [p for p in range(n_pages) if p not in held]
+    assert len(free) == int(need[3]) and (cache.pool.k_pages[free] == 3.0).all()
+    # as many steps of both as the pages allow: the second sequence starts from nothing and needs a page per layer at once
     x = normal(1, N, Hkv, d)
-    cache.append(2, x, x)
-    changed = (cache.pool.k_pages != before).flatten(1).any(1).nonzero().flatten().tolist()
-    assert changed == [s // page for s in slots[2::3] if s >= 0]
+    refused = 0
+    for step in range(3 * page * int(need[3])):
+        lens, left = cache.lens.view(N, L).clone(), int(cache.free_state[1])
+        before = cache.pool.k_pages.clone()
+        got = cache.step()
+        want, left_now = [], left
+        for n in lens.tolist():
+            ask = sum(m % page == 0 for m in n)
+            fits = max(n) < cache.max_blocks * page and ask <= left_now
+            want.append([int(fits)] * L)
+            left_now -= ask if max(n) < cache.max_blocks * page else 0
+        assert got.tolist() == want, step
+        assert torch.equal(cache.lens.view(N, L), lens + got)
+        cache.append(2, x, x)
+        slots = cache.slots[2::L, 0].tolist()
+        assert [t >= 0 for t in slots] == [bool(w[2]) for w in want]
+        changed = (cache.pool.k_pages != before).flatten(1).any(1).nonzero().flatten().tolist()
+        assert set(changed) <= {t // page for t in slots if t >= 0}
+        cache.pool.k_pages.copy_(before)
+        refused += want.count([0] * L)
+        if refused >= 3:
+            break
+    assert refused >= 3
+    cache.release([0])
+    assert cache.step(torch.tensor([0, 1], device=DEV)).tolist() == [[0] * L, [1] * L]      # asked for again, with room
 
 
 def test_graph_replays_and_streams():

@@ -25,6 +25,16 @@ def test_pages_are_conserved_and_held_once(page, n_pages, seed):
             assert (slots[r] >= 0).sum() == min(2, max(0, granted[r]))
 
 
+def test_rows_granted_together_are_a_whole_or_nothing():
+    table, ring = np.full((4, 3), -1), np.arange(5)
+    lens, table, ring, state, slots, granted = P.page_update([0, 0, 0, 0], [16, 17, 16, 17], table, ring, [0, 5], 16, 1, rows_per_seq=2)
+    assert granted.tolist() == [16, 17, 0, 0] and lens.tolist() == [16, 17, 0, 0] and state.tolist() == [3, 2]
+    assert table[0, 0] == 0 and table[1, :2].tolist() == [1, 2] and (table[2:] == -1).all()
+    # the first sequence asks for more than a table holds and needs no pages then; a row of the second has ended
+    lens, table, ring, state, slots, granted = P.page_update(lens, [1, 48, 3, -1], table, ring, state, 16, 1, rows_per_seq=2)
+    assert granted.tolist() == [0, 0, 3, -1] and lens.tolist() == [16, 17, 3, 0] and state.tolist() == [4, 1] and slots[2, 0] == 3 * 16
+
+
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_rotation_is_a_product_of_complex_numbers(interleaved):
     rng = np.random.default_rng(4)

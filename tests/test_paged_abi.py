@@ -82,6 +82,7 @@ def _update(lib, kw=None, ptrs=None, ws=None, ws_bytes=1 << 20):
 
 def test_page_update_refuses(lib):
     for kw, want in ((dict(n_pages=0), INVALID), (dict(n_rows=0), INVALID), (dict(max_blocks=0), INVALID), (dict(max_new=-1), INVALID),
+                     (dict(rows_per_seq=-1), INVALID), (dict(rows_per_seq=3), INVALID), (dict(rows_per_seq=8), INVALID),
                      (dict(n_pages=1 << 31), UNSUPPORTED), (dict(page_size=20), UNSUPPORTED), (dict(n_rows=65537), UNSUPPORTED),
                      (dict(n_rows=65536, max_blocks=32768), UNSUPPORTED), (dict(max_blocks=1 << 25), UNSUPPORTED)):
         assert _update(lib, kw) == want, kw
