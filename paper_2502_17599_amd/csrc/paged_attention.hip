@@ -20,7 +20,7 @@ namespace meda {
 
 constexpr int kAttThreads = kLocateThreads, kAttWaves = kAttThreads / 64;
 constexpr int kBlock = 16;        // positions of one matrix instruction; they lie in one page
-constexpr int kMinUnits = 4;      // a workgroup's share, at least: a step per wave (kFineShares: or two)
+constexpr int kMinUnits = 4;      // a workgroup's share, at least: a step per wave
 constexpr int kMaxGroup = 16;     // query heads per kv head
 // positions of a unit, a step of one wave: two blocks, of 4-byte rows one (as many bytes)
 constexpr int unit_positions(int bytes) { return bytes == 4 ? kBlock : 2 * kBlock; }
@@ -38,7 +38,6 @@ struct PagedArgs {
   long long table_stride, len_stride;
   int R, Hq, Hkv, G, max_blocks;
   int cut_by_pair;
-  unsigned fine_shares;    // up to so many shares may be of kMinUnits units
   float scale_log2;
 };
 
@@ -404,16 +403,14 @@ struct WavePiece {
   bool ends;    // slot 0: the pair ends in this wave
 };
 
-// Workgroups per CU, and waves per SIMD: three where registers and LDS allow it.  All workgroups of a launch are at work at
-// once, each on one share.  (64 requests, 435 MB: 88 us with two per CU, 86 with three; with two and three rounds of shorter
-// shares 104 and 111 instead of 99, before the pages of many steps were loaded at once: the workgroups' searches and the joins
-// cost more than the evener end gained.  Rows of 64 elements, four per CU: three fp32 requests 41.6 us, three per CU 40.1.)
-constexpr int groups_per_cu(int d, int gp) { return d == 128 && gp == 16 ? 2 : 3; }
-constexpr int kCus = 256;
-// Few pairs are cut into many pieces: past this number of shares a wave takes two steps rather than one or two, as the others
-// would wait for it, and the join has fewer pieces to read (one request of 30000 positions, 4 heads: 768 shares 24.9 us, 469
-// 21.7).  Many pairs are cut into few pieces anyhow (272 pairs of 26 to 871 fp32 positions: 768 shares 19.9 us, 540 20.9).
-constexpr int kFineShares = 2 * kCus, kFewPairs = 64;
+// Workgroups per CU, and waves per SIMD.  All workgroups of a launch are at work at once, each on one share: two per CU have
+// enough bytes on their way, with fewer pieces to join than three and no register spilled (40 fp32 requests of 150 to 12000
+// positions 87 us with two, 98 with three; 64 requests, 435 MB 85.2 and 85.9; one of 30000 positions, whose waves then take two
+// steps each instead of one or two, 20.5 and 24.9; 2000 of 10 to 2000 87.7 and 89.9), except for 8-bit rows of 64 elements, of
+// which a step is 4 KB (112 MB: 37.6 us with two, 35.6 with three).  Several rounds of shorter shares cost more in searches
+// and joins than the evener end gains.
+constexpr int groups_per_cu(int d, bool fp8) { return fp8 && d == 64 ? 3 : 2; }
+constexpr int kCus = 256, kFewPairs = 64;
 
 // Four columns of a row of out; a sum of weights of zero (every page is missing) gives zeros.
 __device__ __forceinline__ void store4(char* dst, const float (&x)[4], float) {
@@ -439,7 +436,7 @@ __device__ __forceinline__ float4 either(bool first, const float4& x, const floa
 
 // grid: groups_per_cu workgroups for every CU, or fewer (a share of kMinUnits units for each of the most that there can be).
 template <typename T, int D, int GP, bool FP8>
-__global__ void __launch_bounds__(kAttThreads, (groups_per_cu(D, GP))) paged_attention_kernel(PagedArgs a) {
+__global__ void __launch_bounds__(kAttThreads, (groups_per_cu(D, FP8))) paged_attention_kernel(PagedArgs a) {
   using At = Attend<T, D, GP, FP8>;
   __shared__ __align__(16) float red_o[kAttWaves][2][GP][D];
   __shared__ float red_m[kAttWaves][2][GP], red_z[kAttWaves][2][GP];
@@ -452,8 +449,7 @@ __global__ void __launch_bounds__(kAttThreads, (groups_per_cu(D, GP))) paged_att
   const RowOfUnit at = locate_row(
       a.R, a.Hkv, units,
       [&](unsigned total) {
-        const unsigned fine = min((total + kMinUnits - 1) / kMinUnits, a.fine_shares);
-        const unsigned shares = min(max(fine, (total + 2 * kMinUnits - 1) / (2 * kMinUnits)), gridDim.x);
+        const unsigned shares = min((total + kMinUnits - 1) / kMinUnits, gridDim.x);
         if (id >= (int)shares) return;
         cut_in = Shares(total, shares);
         share = cut_in.first(id);
@@ -590,7 +586,7 @@ __global__ void __launch_bounds__(kAttThreads, (groups_per_cu(D, GP))) paged_att
 // 2000 pairs of up to 300 43.5 and 28.9).
 constexpr int kPairBytes = 320 << 10, kFewPairBytes = 208 << 10, kPairPositions = 512;
 template <typename T, int D, int GP, bool FP8, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, (WAVES == 4 ? groups_per_cu(D, GP) : 2)) paged_pair_kernel(PagedArgs a) {
+__global__ void __launch_bounds__(64 * WAVES, (WAVES == 4 ? groups_per_cu(D, FP8) : 2)) paged_pair_kernel(PagedArgs a) {
   using At = Attend<T, D, GP, FP8>;
   __shared__ __align__(16) float red_o[WAVES][GP][D];
   __shared__ float red_m[WAVES][GP], red_z[WAVES][GP];
@@ -621,9 +617,10 @@ __global__ void __launch_bounds__(64 * WAVES, (WAVES == 4 ? groups_per_cu(D, GP)
 }
 
 // grid (pairs or shares, G): joins the pieces of the (row, kv head) that blockIdx.x names, one query head each.  Four columns per
-// thread, kJoinLanes pieces side by side and eight of each on their way together: 128 pieces take two rounds, or one with 64
-// columns per row.  (256 pairs of seven heads, most of them cut in two or three: 4.6 us, 6.0 with 512 threads; four pairs cut
-// into 192 pieces 6.0 and 5.4.  One column per thread, two pieces side by side: twice as long.)
+// thread, kJoinLanes pieces side by side and eight of each on their way together: 128 pieces take two rounds with 256 threads
+// and one with 512, which pairs of that many pieces get (a step over one pair of 30000 positions in 234 pieces 15.0 us with 256
+// and 13.8 with 512 threads, four pairs in 128 each 20.9 and 20.3; eight in 96 11.5 and 12.1; 256 pairs cut in two or three 80
+// and 82).  One column per thread, two pieces side by side: twice as long.
 constexpr int kJoinPieces = 128;
 template <typename T, int D, int kJoinThreads>
 __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a) {
@@ -719,7 +716,7 @@ static meda_status make_paged_plan(const meda_page_pool* pool, const meda_paged_
   if (p->q_stride * elt % 16 || p->out_stride * elt % 16) return MEDA_ERR_INVALID_ARG;
   const int64_t unit = unit_positions(elt), units = (most + unit - 1) / unit * pool->n_kv_heads;   // of one row, at most
   pl->GP = G <= 1 ? 1 : (G <= 2 ? 2 : (G <= 4 ? 4 : (G <= 8 ? 8 : 16)));
-  const int64_t most_groups = kCus * groups_per_cu(pool->head_dim, pl->GP);
+  const int64_t most_groups = kCus * groups_per_cu(pool->head_dim, pool->dtype == MEDA_E4M3);
   const int64_t shares = units > most_groups * kMinUnits ? most_groups : (units * p->n_rows + kMinUnits - 1) / kMinUnits;
   pl->groups = (int)(shares < most_groups ? shares : most_groups);
   pl->pair_waves = 0;
@@ -797,9 +794,7 @@ meda_status meda_paged_attention(const meda_page_pool* pool, const meda_paged_pa
   a.table_stride = p.table_stride ? p.table_stride : p.max_blocks;
   a.len_stride = p.len_stride ? p.len_stride : 1;
   a.R = p.n_rows; a.Hq = p.n_q_heads; a.Hkv = pool->n_kv_heads; a.G = a.Hq / a.Hkv; a.max_blocks = p.max_blocks;
-  const int64_t pairs = (int64_t)p.n_rows * pool->n_kv_heads;
-  a.cut_by_pair = pairs <= pl.groups;
-  a.fine_shares = pairs <= kFewPairs ? kFineShares : pl.groups;
+  a.cut_by_pair = (int64_t)p.n_rows * pool->n_kv_heads <= pl.groups;
   const double scale = p.softmax_scale > 0.0f ? (double)p.softmax_scale : 1.0 / sqrt((double)pool->head_dim);
   a.scale_log2 = (float)(scale * 1.4426950408889634074);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
