@@ -99,15 +99,15 @@ struct PlanTotals {
 //
 // Rows in groups: a row that does not fit into its table marks its group, whose needs then do not count; what is granted
 // follows from the sum at the group's end, once every row's place in the scan is known: put(r, plan) keeps it as it is then
-// (count: what was asked for), get(r) gives it back.  (512 rows, a token each: 4.2 us, in groups of 32 5.0.)
-template <typename Keep, typename Put, typename Get>
+// (count: what was asked for), get(r) gives it back.  (512 rows, a token each: 3.8 us, in groups of 32 4.8.)
+template <bool GROUPS, typename Keep, typename Put, typename Get>
 __device__ __forceinline__ PlanTotals plan_rows(const PageUpdate& a, Keep keep, Put put, Get get) {
   __shared__ int wave_need[kPlanThreads / 64], wave_give[kPlanThreads / 64];
   __shared__ unsigned refused[kMaxRows / 2 / 32];   // a bit per group
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, groups = a.R / a.group;
   auto refuse = [&](int g) { atomicOr(&refused[g >> 5], 1u << (g & 31)); };
   auto is_refused = [&](int g) { return ((refused[g >> 5] >> (g & 31)) & 1u) != 0u; };
-  if (a.group > 1) {
+  if constexpr (GROUPS) {
     for (int i = tid; i < (groups + 31) / 32; i += kPlanThreads) refused[i] = 0u;
     __syncthreads();
     for (int r = tid; r < a.R; r += kPlanThreads) {
@@ -123,7 +123,7 @@ __device__ __forceinline__ PlanTotals plan_rows(const PageUpdate& a, Keep keep, 
     const int r = base + tid;
     RowNeed n{0, 0, 0, 0, 0, false};
     if (r < a.R) n = row_need(a, r);
-    if (a.group > 1 && r < a.R && is_refused(r / a.group)) {
+    if (GROUPS && r < a.R && is_refused(r / a.group)) {
       n.fits = false;
       n.need = 0;
     }
@@ -142,7 +142,7 @@ __device__ __forceinline__ PlanTotals plan_rows(const PageUpdate& a, Keep keep, 
       need_before += wave_need[w];
       give_before += wave_give[w];
     }
-    if (a.group > 1) {
+    if constexpr (GROUPS) {
       if (r < a.R) put(r, RowPlan{need_to - n.need, give_to - n.give, n.len, n.want < 0 ? -1 : (n.fits ? n.want : 0)});
     } else if (r < a.R) {
       const bool grant = n.fits && (n.need == 0 || need_to <= t.free);
@@ -150,7 +150,7 @@ __device__ __forceinline__ PlanTotals plan_rows(const PageUpdate& a, Keep keep, 
       keep(r, RowPlan{need_to - n.need, give_to - n.give, n.len, n.want < 0 ? -1 : (grant ? n.want : 0)});
     }
   }
-  if (a.group > 1) {
+  if constexpr (GROUPS) {
     __syncthreads();
     for (int g = tid; g < groups; g += kPlanThreads) {
       const int from = get(g * a.group).base, to = g + 1 < groups ? get((g + 1) * a.group).base : need_before;
@@ -189,9 +189,10 @@ __device__ __forceinline__ void write_state(const PageUpdate& a, const PlanTotal
 // (the row of the n-th page taken or given back is searched in the scan's sums).  grid: one workgroup, or, where lens_out and
 // state_out are arrays of their own, any number: every workgroup scans all rows and takes a part of the entries.
 constexpr int kFusedRows = 2048;
+template <bool GROUPS>
 __global__ void __launch_bounds__(kPlanThreads) page_update_kernel(PageUpdate a) {
   __shared__ RowPlan rows[kFusedRows];
-  const PlanTotals t = plan_rows(
+  const PlanTotals t = plan_rows<GROUPS>(
       a,
       [&](int r, const RowPlan& p) {
         rows[r] = p;
@@ -226,10 +227,11 @@ __global__ void __launch_bounds__(kPlanThreads) page_update_kernel(PageUpdate a)
 }
 
 // More rows, or many slots beside lengths that are updated in place: the scan by itself, plan[r] for every row ...
+template <bool GROUPS>
 __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(PageUpdate a) {
   int head, free;
   ring_state(a, head, free);
-  const PlanTotals t = plan_rows(
+  const PlanTotals t = plan_rows<GROUPS>(
       a,
       [&](int r, const RowPlan& p) {
         a.plan[r] = make_int4(ring_at(a, head, p.count > 0 ? p.base : 0), ring_at(a, head, (long long)free + p.behind), p.len, p.count);
@@ -264,10 +266,12 @@ static hipError_t launch_page_update(const PageUpdate& a, hipStream_t s) {
   if (a.R <= kFusedRows && (entries <= kAloneSlots || (!in_place && entries < (1ll << 31)))) {
     long long groups = entries <= kAloneSlots ? 1 : (entries + 4 * kPlanThreads - 1) / (4 * kPlanThreads);
     if (groups > 256) groups = 256;
-    hipLaunchKernelGGL(page_update_kernel, dim3((unsigned)groups), dim3(kPlanThreads), 0, s, a);
+    if (a.group > 1) hipLaunchKernelGGL(page_update_kernel<true>, dim3((unsigned)groups), dim3(kPlanThreads), 0, s, a);
+    else hipLaunchKernelGGL(page_update_kernel<false>, dim3((unsigned)groups), dim3(kPlanThreads), 0, s, a);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL(page_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
+  if (a.group > 1) hipLaunchKernelGGL(page_plan_kernel<true>, dim3(1), dim3(kPlanThreads), 0, s, a);
+  else hipLaunchKernelGGL(page_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int longest = a.max_new > a.max_blocks ? a.max_new : a.max_blocks;
