@@ -225,7 +225,7 @@ def test_refusals():
     import paper_2502_17599_amd as pkg
     L, Hq, Hkv, d = 2, 4, 2, 64
     _, compressed, T = _prompts(1, L, Hq, Hkv, d, "f32", 0, 32, 2 * 100, 90)
-    for bad in (dict(n_seqs=0), dict(n_layers=0), dict(page_size=17), dict(max_len=0)):
+    for bad in (dict(n_seqs=0), dict(n_layers=0), dict(page_size=17), dict(max_len=0), dict(n_seqs=32769), dict(max_len=1 << 35), dict(n_pages=0)):
         with pytest.raises(ValueError):
             pkg.PagedCache(**dict(dict(n_seqs=1, n_layers=L, n_q_heads=Hq, n_kv_heads=Hkv, head_dim=d, max_len=T, n_pages=9), **bad))
     cache = pkg.PagedCache(1, L, Hq, Hkv, d, max_len=T, n_pages=40, page_size=16, dtype=torch.float32)
