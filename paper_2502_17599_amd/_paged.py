@@ -497,8 +497,8 @@ class PagedCache:
                  device="cuda:0"):
         if n_seqs < 1 or n_layers < 1 or max_len < 1 or page_size not in PAGE_SIZES:
             raise ValueError(f"expected sequences, layers, a length and a page size of {PAGE_SIZES}")
-        if n_seqs * n_layers > 65536 or n_seqs * n_layers * -(-max_len // page_size) > 1 << 30:
-            raise ValueError("more than 65536 layers of sequences, or 2^30 blocks of them")
+        if max_len > 1 << 29 or n_seqs * n_layers > 65536 or n_seqs * n_layers * -(-max_len // page_size) > 1 << 30:
+            raise ValueError("more than 2^29 positions, 65536 layers of sequences, or 2^30 blocks of them")
         self.pool = PagePool.empty(n_pages, n_kv_heads, page_size, head_dim, dtype, device)
         dev = self.pool.device
         self.n_seqs, self.n_layers, self.n_q_heads, self.rope = n_seqs, n_layers, n_q_heads, rope
