@@ -110,7 +110,7 @@ class PagePool:
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: Optional[torch.Tensor] = None,
                  v_scales: Optional[torch.Tensor] = None):
-        if k_pages.dim() != 4 or k_pages.dtype not in (torch.float32, torch.bfloat16, torch.uint8) or not k_pages.is_cuda:
+        if k_pages.dim() != 4 or k_pages.dtype not in (torch.float32, torch.bfloat16, torch.uint8):
             raise ValueError("k_pages: expected a float32, bfloat16 or uint8 tensor [n_pages][n_kv_heads][page_size][head_dim] on the GPU")
         n, heads, page, d = k_pages.shape
         if n < 1 or heads < 1:
@@ -120,6 +120,9 @@ class PagePool:
                     or not t[0].is_contiguous() or (n > 1 and t.stride(0) != k_pages.stride(0))):
                 raise ValueError(f"{name}: expected {k_pages.dtype} {tuple(k_pages.shape)} on {k_pages.device}, every page "
                                  "contiguous, K and V pages the same distance apart")
+        # (a page that is repeated has a distance of 0, which the library takes for that of pages next to each other)
+        if n > 1 and k_pages.stride(0) < heads * page * d:
+            raise ValueError(f"k_pages, v_pages: pages of {heads * page * d} elements lie {k_pages.stride(0)} apart")
         if page not in PAGE_SIZES:
             raise ValueError(f"page_size {page}: expected one of {PAGE_SIZES}")
         if k_pages.dtype == torch.uint8:
@@ -127,6 +130,8 @@ class PagePool:
                 _want(name, t, (n, heads, page), torch.float32, k_pages.device)
         elif k_scales is not None or v_scales is not None:
             raise ValueError("scales belong to uint8 pages")
+        if not k_pages.is_cuda:
+            raise ValueError("k_pages, v_pages: expected tensors on the GPU")
         self.k_pages, self.v_pages, self.k_scales, self.v_scales = k_pages, v_pages, k_scales, v_scales
         self.device, self.page_size, self.n_kv_heads, self.head_dim, self.n_pages = k_pages.device, page, heads, d, n
         # the type of the rows that are written to the pages and of the queries that read them
