@@ -257,7 +257,8 @@ __global__ void __launch_bounds__(256) page_fill_kernel(PageUpdate a) {
     const int need = (int)(((long long)len + count + page - 1) >> a.page_log2) - held;
     for (int j = at; j < need; j += step) take_page(a, r, plan.x, held, j);
   }
-  for (int i = at; i < a.max_new; i += step) write_slot(a, r, plan.x, held, len, count, i);
+  // (unsigned: a step behind the last of nearly 2^31 slots is past the range of int)
+  for (unsigned i = at; i < (unsigned)a.max_new; i += step) write_slot(a, r, plan.x, held, len, count, (int)i);
 }
 
 static hipError_t launch_page_update(const PageUpdate& a, hipStream_t s) {
@@ -275,7 +276,7 @@ static hipError_t launch_page_update(const PageUpdate& a, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int longest = a.max_new > a.max_blocks ? a.max_new : a.max_blocks;
-  int parts = (longest + 1023) / 1024;
+  int parts = (longest - 1) / 1024 + 1;
   if (parts > 16) parts = 16;
   hipLaunchKernelGGL(page_fill_kernel, dim3(a.R, parts), dim3(256), 0, s, a);
   return hipGetLastError();
