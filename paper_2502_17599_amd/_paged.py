@@ -570,10 +570,15 @@ class PagedCache:
         return self.decoder(q, table, lens, out)
 
     def release(self, seqs) -> None:
-        """The sequences' pages go back to the pool, their lengths become 0."""
-        self._new.zero_()
+        """The sequences' pages go back to the pool, their lengths become 0.  A slot that the last step gave them is theirs no
+        longer: what is appended for them before the next step is not written."""
+        seqs = list(seqs)
         for s in seqs:
             if not 0 <= s < self.n_seqs:
                 raise ValueError(f"sequence {s}: expected one of {self.n_seqs}")
+        self._new.zero_()
+        slots = self.slots.view(self.n_seqs, self.n_layers)
+        for s in seqs:
             self._new[s].fill_(-1)
+            slots[s].fill_(-1)
         self._update()
