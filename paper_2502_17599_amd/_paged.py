@@ -104,6 +104,14 @@ def _want_no_overlap(name, out, other_name, other, may_be_same):
     raise ValueError(f"{name} overlaps {other_name}")
 
 
+def _pages_apart(k, v):
+    """Whether no page of k shares memory with one of v: all of one behind the other's, or in the gaps between them."""
+    a, b, size = k.data_ptr(), v.data_ptr(), k[0].numel() * k.element_size()
+    step = k.stride(0) * k.element_size()
+    extent = (k.shape[0] - 1) * step + size
+    return a + extent <= b or b + extent <= a or (k.shape[0] > 1 and (b - a) % step >= size and (a - b) % step >= size)
+
+
 class PagePool:
     """Pages of K and V [n_pages][n_kv_heads][page_size][head_dim] (any distance from page to page, the same for both),
     for 8-bit pages (uint8 codes) with one scale per row [n_pages][n_kv_heads][page_size]."""
@@ -130,6 +138,8 @@ class PagePool:
                 _want(name, t, (n, heads, page), torch.float32, k_pages.device)
         elif k_scales is not None or v_scales is not None:
             raise ValueError("scales belong to uint8 pages")
+        if not _pages_apart(k_pages, v_pages) or (k_scales is not None and not _pages_apart(k_scales, v_scales)):
+            raise ValueError("K and V pages, and their scales, must not share memory")
         if not k_pages.is_cuda:
             raise ValueError("k_pages, v_pages: expected tensors on the GPU")
         self.k_pages, self.v_pages, self.k_scales, self.v_scales = k_pages, v_pages, k_scales, v_scales

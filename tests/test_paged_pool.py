@@ -39,3 +39,26 @@ def test_what_was_taken_still_is_up_to_the_device(dtype):
     one = [_pages(dtype, 1).as_strided((1, 2, 16, 64), (0, 16 * 64, 64, 1)) for _ in range(2)]
     with pytest.raises(ValueError, match="on the GPU"):
         pkg.PagePool(*one, *_scales(dtype, 1))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_k_and_v_pages_that_share_memory_are_refused(dtype):
+    """A token's k and v would be written to the same place."""
+    x, size = torch.zeros(20 * 2 * 16 * 64, dtype=dtype), 2 * 16 * 64
+
+    def pages(first, step, n=5):
+        return x[first:].as_strided((n, 2, 16, 64), (step, 16 * 64, 64, 1))
+    scales = _scales(dtype)
+    for k, v in ((pages(0, size), pages(0, size)), (pages(0, size), pages(size, size)), (pages(0, 3 * size), pages(2 * size + 16, 3 * size)),
+                 (pages(size - 16, 2 * size), pages(0, 2 * size)), (pages(0, 3 * size), pages(6 * size, 3 * size)),
+                 (pages(0, size, 1), pages(64, size, 1))):
+        for a, b in ((k, v), (v, k)):
+            with pytest.raises(ValueError, match="share memory"):
+                pkg.PagePool(a, b, *_scales(dtype, k.shape[0]))
+    for k, v in ((pages(0, size), pages(5 * size, size)), (pages(0, 3 * size), pages(2 * size, 3 * size)), (pages(0, size, 1), pages(size, size, 1))):
+        for a, b in ((k, v), (v, k)):
+            with pytest.raises(ValueError, match="on the GPU"):
+                pkg.PagePool(a, b, *_scales(dtype, k.shape[0]))
+    if scales:
+        with pytest.raises(ValueError, match="share memory"):
+            pkg.PagePool(_pages(dtype), _pages(dtype), scales[0], scales[0])
