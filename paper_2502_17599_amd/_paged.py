@@ -139,7 +139,7 @@ class PagePool:
         elif k_scales is not None or v_scales is not None:
             raise ValueError("scales belong to uint8 pages")
         if not _pages_apart(k_pages, v_pages) or (k_scales is not None and not _pages_apart(k_scales, v_scales)):
-            raise ValueError("K and V pages, and their scales, must not share memory")
+            raise ValueError("k_pages and v_pages, k_scales and v_scales: must not share memory")
         if not k_pages.is_cuda:
             raise ValueError("k_pages, v_pages: expected tensors on the GPU")
         self.k_pages, self.v_pages, self.k_scales, self.v_scales = k_pages, v_pages, k_scales, v_scales
