@@ -39,6 +39,23 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+class _Kept:
+    """Memory that an object keeps from call to call.  The allocator knows the stream where it was made; it has to hear of
+    every other one that works with it, or it would give the memory away, once the object is gone, while kernels of that
+    stream still use it."""
+
+    def __init__(self, device: int, tensors):
+        self._device, self._tensors = device, [t for t in tensors if t is not None]
+        self._streams = {torch._C._cuda_getCurrentRawStream(device)}
+
+    def used_on(self, stream) -> None:
+        raw = torch._C._cuda_getCurrentRawStream(self._device) if stream is None else stream.cuda_stream
+        if raw not in self._streams:
+            for t in self._tensors:
+                t.record_stream(torch.cuda.current_stream(self._device) if stream is None else stream)
+            self._streams.add(raw)
+
+
 # A call of a kind that was checked before (the same shapes, strides, types and devices) is not checked again: half of the
 # time of a small call went into it.  What an entry holds depends on nothing else, addresses least of all.  (Keys of the
 # calls of every layer are spelled out: with a function per tensor an append of 64 tokens took 7.4 us instead of 7.1, a step of
@@ -385,6 +402,7 @@ class PagedDecoder:
         self.workspace, self._workspace_bytes = torch.empty(need, dtype=torch.uint8, device=pool.device), need
         self._calls: dict = {}     # parameters of calls by the shapes and strides of their tensors, as in _checked
         self.out = torch.empty((n_rows, n_q_heads, pool.head_dim), dtype=dt, device=pool.device)
+        self._kept = _Kept(pool.index, (self.workspace, self.out))
 
     def __call__(self, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, out: Optional[torch.Tensor] = None,
                  stream=None) -> torch.Tensor:
@@ -402,6 +420,7 @@ class PagedDecoder:
         pool, pq, po = self.pool, q.data_ptr(), out.data_ptr()
         if pq < po + out_bytes and po < pq + q_bytes:
             _want_no_overlap("out", out, "q", q, False)
+        self._kept.used_on(stream)
         _call(load_library().meda_paged_attention, pool.index, stream, pool.ref, params, pq, table.data_ptr(), lens.data_ptr(), po,
               self.workspace.data_ptr(), self._workspace_bytes)
         return out
@@ -527,6 +546,9 @@ class PagedCache:
         self._new = torch.zeros((n_seqs, n_layers), dtype=torch.int32, device=dev)
         self._workspace = torch.empty(meda_page_update_workspace_bytes(rows), dtype=torch.uint8, device=dev)
         self.decoder = PagedDecoder(self.pool, n_seqs, n_q_heads, self.max_blocks, None, softmax_scale)
+        p = self.pool
+        self._kept = _Kept(p.index, (p.k_pages, p.v_pages, p.k_scales, p.v_scales, self.table, self.lens, self.granted, self.slots,
+                                     self.free_ring, self.free_state, self._new, self._workspace))
 
     def _update(self, slots=None):
         meda_page_update(self.lens, self._new.view(-1), self.table, self.free_ring, self.free_state, self.pool.page_size,
@@ -552,6 +574,7 @@ class PagedCache:
     def step(self, active: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Room for one token per active sequence (int32 or bool [n_seqs]; all without it); returns what was granted,
         [n_seqs][n_layers]."""
+        self._kept.used_on(None)
         if active is None:
             self._new.fill_(1)
         else:
@@ -571,11 +594,13 @@ class PagedCache:
                positions: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
         """k, v [n_seqs][Hkv][d] of the step's tokens enter the layer; returns q [n_seqs][Hq][d].  k and q are rotated by
         ``positions`` where the cache has a plan of the rotation; without one they are taken as they are."""
+        self._kept.used_on(None)
         return meda_paged_append(self.pool, k, v, self._rows(layer)[2], q, positions, self.rope, q_out)
 
     def attend(self, layer: int, q: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of q [n_seqs][Hq][d] over the layer's positions, the step's own included (without ``out`` the result
         lies in a buffer that the next call overwrites)."""
+        self._kept.used_on(None)
         table, lens, _ = self._rows(layer)
         return self.decoder(q, table, lens, out)
 
@@ -586,6 +611,7 @@ class PagedCache:
         for s in seqs:
             if not 0 <= s < self.n_seqs:
                 raise ValueError(f"sequence {s}: expected one of {self.n_seqs}")
+        self._kept.used_on(None)
         self._new.zero_()
         slots = self.slots.view(self.n_seqs, self.n_layers)
         for s in seqs:

@@ -27,7 +27,7 @@ def test_a_released_sequence_writes_into_nobodys_pages(how):
         to = 1
     else:
         to = 0
-    assert torch.equal(cache.admit(to, compressed).reshape(-1), compressed.layer_len)
+    assert torch.equal(cache.admit(to, compressed), compressed.layer_len)
     assert int(cache.free_state[1]) == 0 and torch.equal(cache.slots[2 * L:], kept) and (cache.slots[:2 * L] == -1).all()
     x = normal(7, 3, Hkv, d)
     for l in range(L):
