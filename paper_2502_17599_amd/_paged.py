@@ -14,6 +14,8 @@ ROTARY_INTERLEAVED = 1
 ROTARY_INVERSE = 2
 PAGE_SIZES = (16, 32, 64, 128, 256)
 _E4M3 = 2
+# Rows that a kernel writes count as changed in place: a graph that has kept them for its backward pass then says so.
+_written = torch.autograd.graph.increment_version
 
 
 def _p(t: Optional[torch.Tensor]):
@@ -37,6 +39,14 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _no_graph(*tensors):
+    """The kernels record nothing for a backward pass: a tensor that needs one is refused, not cut off in silence."""
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            raise ValueError("a tensor requires grad: gradients are not recorded here, call under torch.no_grad() or with detached "
+                             "tensors (the gradient of meda_rotary is the same call with inverse=True)")
 
 
 class _Kept:
@@ -157,6 +167,7 @@ class PagePool:
             raise ValueError("scales belong to uint8 pages")
         if not _pages_apart(k_pages, v_pages) or (k_scales is not None and not _pages_apart(k_scales, v_scales)):
             raise ValueError("k_pages and v_pages, k_scales and v_scales: must not share memory")
+        _no_graph(k_pages, v_pages, k_scales, v_scales)
         if not k_pages.is_cuda:
             raise ValueError("k_pages, v_pages: expected tensors on the GPU")
         self.k_pages, self.v_pages, self.k_scales, self.v_scales = k_pages, v_pages, k_scales, v_scales
@@ -219,7 +230,9 @@ def meda_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Ten
                 stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """Rotary positions of q [T][Hq][d] and k [T][Hk][d] (any strides with contiguous rows; ``x.transpose(0, 1)`` of an
     [H][T][d] array is such a view).  The outputs may be the inputs; without them new ones are made.  ``inverse`` turns
-    back: the gradient of the rotation."""
+    back: the gradient of the rotation (it is not recorded: tensors that require grad are refused where grad mode is on)."""
+    if torch.is_grad_enabled():
+        _no_graph(q, k, q_out, k_out)
     key = ("rotary", None if rope is None else rope.key, inverse, q.shape, q.stride(), q.dtype, q.get_device(),
            positions if positions is None else (positions.shape, positions.stride(), positions.dtype, positions.get_device()),
            k if k is None else (k.shape, k.stride(), k.dtype, k.get_device()),
@@ -242,6 +255,10 @@ def meda_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Ten
                 _want_no_overlap(name, out, "k", k, name == "k_out")
     if pko is not None and po < pko + ext[3] and pko < po + ext[2]:
         _want_no_overlap("q_out", q_out, "k_out", k_out, False)
+    if new_q is None:
+        _written(q_out)
+    if new_k is None and k_out is not None:
+        _written(k_out)
     _call(load_library().meda_rotary, dev, stream, params, pq, pk, positions.data_ptr(), rope.inv_freq.data_ptr(), _p(rope.axis), po, pko)
     return q_out, k_out
 
@@ -284,6 +301,8 @@ def meda_paged_append(pool: PagePool, k: torch.Tensor, v: torch.Tensor, slots: t
                       stream=None) -> Optional[torch.Tensor]:
     """Writes k, v [M][Hkv][d] of new tokens to their ``slots`` (int64 [M], -1: none), k rotated where a plan is given;
     returns q [M][Hq][d] rotated alike (``q_out``, which may be q)."""
+    if torch.is_grad_enabled():
+        _no_graph(k, v, q, q_out)
     key = ("append", pool.key, None if rope is None else rope.key, k.shape, k.stride(), k.dtype, k.get_device(),
            v.shape, v.stride(), v.dtype, v.get_device(), slots.shape, slots.stride(), slots.dtype, slots.get_device(),
            q if q is None else (q.shape, q.stride(), q.dtype, q.get_device()),
@@ -301,6 +320,8 @@ def meda_paged_append(pool: PagePool, k: torch.Tensor, v: torch.Tensor, slots: t
             a = t.data_ptr()
             if po < a + n and a < po + ext[3]:
                 _want_no_overlap("q_out", q_out, name, t, name == "q")
+    if new_q is None and q_out is not None:
+        _written(q_out)
     turn = (None, None, None) if rope is None else (positions.data_ptr(), rope.inv_freq.data_ptr(), _p(rope.axis))
     _call(load_library().meda_paged_append, pool.index, stream, pool.ref, params, _p(q), k.data_ptr(), v.data_ptr(), *turn, slots.data_ptr(), po)
     return q_out
@@ -359,6 +380,8 @@ def _want_table(table, lens, device):
 def meda_paged_store(pool: PagePool, cache: CompressedCache, table: torch.Tensor, lens: torch.Tensor, stream=None) -> None:
     """Moves the caches that a call of meda_compress returned to pages: row n * L + l of ``table`` and ``lens`` (the lengths
     that meda_page_update granted) belongs to layer l of sequence n."""
+    if torch.is_grad_enabled():
+        _no_graph(cache.k_out, cache.v_out)
     key = ("store", pool.key, cache.n_kv_heads, _kind(cache.k_out), _kind(cache.v_out), _kind(cache.layer_len), _kind(cache.layer_off),
            _kind(table), _kind(lens))
     params = _checked.get(key)
@@ -409,6 +432,8 @@ class PagedDecoder:
         """q [rows][Hq][d] (rows any distance apart) over the pages of ``table`` [rows][blocks]; ``lens`` [rows].  Without
         ``out`` the result lies in a buffer that the next call overwrites."""
         out = self.out if out is None else out
+        if torch.is_grad_enabled():
+            _no_graph(q, out)
         key = (q.shape, q.stride(), q.dtype, q.get_device(), table.shape, table.stride(), table.dtype, table.get_device(),
                lens.shape, lens.stride(), lens.dtype, lens.get_device(), out.shape, out.stride(), out.dtype, out.get_device())
         call = self._calls.get(key)
@@ -420,6 +445,7 @@ class PagedDecoder:
         pool, pq, po = self.pool, q.data_ptr(), out.data_ptr()
         if pq < po + out_bytes and po < pq + q_bytes:
             _want_no_overlap("out", out, "q", q, False)
+        _written(out)
         self._kept.used_on(stream)
         _call(load_library().meda_paged_attention, pool.index, stream, pool.ref, params, pq, table.data_ptr(), lens.data_ptr(), po,
               self.workspace.data_ptr(), self._workspace_bytes)
