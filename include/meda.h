@@ -384,8 +384,8 @@ meda_status meda_paged_store(const meda_page_pool* pool, const meda_store_params
 
 /*
  * Attention of one new token per row over its pages: out = Softmax(q K^T * scale) V over the first lens[r] positions, query
- * head h reading kv head h / (Hq/Hkv); zeros where no position is left or every logit is -inf.  A value of +-inf in a position whose weight does
- * not underflow gives +-inf in its column of out.
+ * head h reading kv head h / (Hq/Hkv); zeros where no position is left or every logit is -inf.  A value of +-inf in a
+ * position whose weight is at least 2^-100 of the largest gives +-inf in its column of out.
  *   q, out   [R][Hq][d]; row r at r * q_stride and r * out_stride elements (0 = Hq * d), multiples of 16 bytes; `dtype`:
  *            MEDA_F32 for pages of MEDA_F32, MEDA_BF16 for pages of MEDA_BF16 and MEDA_E4M3; out does not overlap q
  *   table    row r at r * table_stride (0 = max_blocks); lens: that of row r at r * len_stride (0 = 1)

@@ -247,6 +247,12 @@ __device__ __forceinline__ uint32_t float_to_bf16_rne(float f) {
   const uint32_t u = __float_as_uint(f);
   return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
 }
+// Two floats as bf16, to nearest even (one conversion instruction).
+__device__ __forceinline__ uint32_t floats_to_bf16x2(float a, float b) {
+  typedef float f32x2_t __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
+}
 
 __device__ __forceinline__ uint32_t double_to_bf16_bits(double x) {
   return float_to_bf16_rne(double_to_float_round_odd(x));

@@ -98,10 +98,10 @@ __device__ __forceinline__ UnitPages<BLOCKS> unit_pages(const PagedArgs& a, int 
 // The second product O[row][col] += sum_key P[row][key] V[key][col] contracts over the keys in an order in which its
 // weights are what the lane has.
 //   bf16 and 8 bits (16x16x32): a weight enters as the sum of two bf16 numbers, rows c / GP = 0 and 1 of the product (what the
-// first leaves is exact and not zero, and 2^-16 of the weight is lost at most: a 128th of the output's own rounding), so that
-// groups of up to 8 heads need one instruction per 16 columns; groups of 9 to 16 take two, one per part.  The values are 8
-// keys at d / 16 columns, transposed in registers.  8-bit rows: codes become bf16 exactly, the key's scale multiplies the
-// logit and the value's scale the weight.
+// first leaves is exact and not zero; the second is that to nearest even, which is off by 2^-16 of the weight at most, either
+// way: a 128th of the output's own rounding), so that groups of up to 8 heads need one instruction per 16 columns; groups of 9
+// to 16 take two, one per part.  The values are 8 keys at d / 16 columns, transposed in registers.  8-bit rows: codes become
+// bf16 exactly, the key's scale multiplies the logit and the value's scale the weight.
 //   fp32 (16x16x4): products and sums in fp32.  Four instructions use up the 16 bytes that a lane loads of a key or of a value;
 // the values' column is 4 c + e of 64.  (On the vector unit, with the dot products summed over lanes, groups of 8 and
 // 16 heads were bound by its instructions: 3.9 and 2.0 TB/s.)
@@ -270,15 +270,15 @@ struct Attend {
       uint32_t pa[4], pb[4];
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
-        uint32_t x[2], y[2];
+        float x[2], y[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const float hi = weight_part(w[e + u]), lo = w[e + u] - hi;
-          x[u] = __float_as_uint(GP == 16 || part == 0 ? hi : lo);
-          y[u] = __float_as_uint(lo);
+          const float hi = weight_part(w[e + u]);
+          y[u] = w[e + u] - hi;
+          x[u] = GP == 16 || part == 0 ? hi : y[u];
         }
-        pa[e / 2] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302u);
-        pb[e / 2] = __builtin_amdgcn_perm(y[1], y[0], 0x07060302u);
+        pa[e / 2] = floats_to_bf16x2(x[0], x[1]);   // (the upper part is a bf16 number: it stays as it is)
+        pb[e / 2] = floats_to_bf16x2(y[0], y[1]);
       }
       const bf16x8_t wa = __builtin_bit_cast(bf16x8_t, make_uint4(pa[0], pa[1], pa[2], pa[3]));
       const bf16x8_t wb = __builtin_bit_cast(bf16x8_t, make_uint4(pb[0], pb[1], pb[2], pb[3]));

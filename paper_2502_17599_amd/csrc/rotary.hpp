@@ -41,12 +41,6 @@ __device__ __forceinline__ void rotary_factors(const RotaryPlan& p, const float2
   s = first ? -cs.y : cs.y;
 }
 
-// Two floats as bf16, to nearest even (one conversion instruction).
-__device__ __forceinline__ uint32_t floats_to_bf16x2(float a, float b) {
-  typedef float f32x2_t __attribute__((ext_vector_type(2)));
-  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
-}
 __device__ __forceinline__ uint4 pack_row(const float (&f)[8]) {
   return make_uint4(floats_to_bf16x2(f[0], f[1]), floats_to_bf16x2(f[2], f[3]), floats_to_bf16x2(f[4], f[5]), floats_to_bf16x2(f[6], f[7]));
 }
