@@ -20,14 +20,18 @@ struct RotaryPlan {
 
 // (cos, sin) of pair `pair` at token t.
 // The angle in turns, reduced to [-1/2, 1/2], is a product of doubles: with 32 bits the position 100000 would leave an
-// error of 0.006 rad.  Its error here is 2^-52 of the number of turns.
+// error of 0.006 rad.  Its error here is 2^-52 of the number of turns.  The sine and cosine are those of the angle x rounded
+// to 32 bits; what that leaves, d (2^-26 turns at most), enters by their derivatives, cos(x + d) = cos x - d sin x and
+// sin(x + d) = sin x + d cos x up to d^2 / 2 < 2^-47: two multiply-adds, after which the 32-bit results are those of the 64-bit
+// angle.  (Without them sines and cosines were off by 2^-23.4 rad, and those near zero by far more than a rounding.)
 __device__ __forceinline__ float2 rotary_pair(const RotaryPlan& p, long long t, int pair) {
   const int ax = p.axis ? min((int)p.axis[pair], p.axes - 1) : 0;
   double turns = (double)p.positions[ax * p.pos_stride + t] * p.inv_freq[pair] * 0.15915494309189533577;
   turns -= rint(turns);
+  const float x = (float)turns, d = (float)(turns - (double)x) * 6.2831853071795864769f;
   float sn, cs;
-  sincospif(2.0f * (float)turns, &sn, &cs);
-  return make_float2(cs, sn * p.sign);
+  sincospif(2.0f * x, &sn, &cs);
+  return make_float2(fmaf(-d, sn, cs), fmaf(d, cs, sn) * p.sign);
 }
 
 // Factors of element e of a row, from its token's pairs: out = x * c + partner * s; (1, 0) past the turned elements.
