@@ -301,7 +301,8 @@ def meda_paged_append(pool: PagePool, k: torch.Tensor, v: torch.Tensor, slots: t
                       stream=None) -> Optional[torch.Tensor]:
     """Writes k, v [M][Hkv][d] of new tokens to their ``slots`` (int64 [M], -1: none), k rotated where a plan is given;
     returns q [M][Hq][d] rotated alike (``q_out``, which may be q)."""
-    if torch.is_grad_enabled():
+    if torch.is_grad_enabled() and (k.requires_grad or v.requires_grad or (q is not None and q.requires_grad)
+                                    or (q_out is not None and q_out.requires_grad)):
         _no_graph(k, v, q, q_out)
     key = ("append", pool.key, None if rope is None else rope.key, k.shape, k.stride(), k.dtype, k.get_device(),
            v.shape, v.stride(), v.dtype, v.get_device(), slots.shape, slots.stride(), slots.dtype, slots.get_device(),
@@ -432,7 +433,7 @@ class PagedDecoder:
         """q [rows][Hq][d] (rows any distance apart) over the pages of ``table`` [rows][blocks]; ``lens`` [rows].  Without
         ``out`` the result lies in a buffer that the next call overwrites."""
         out = self.out if out is None else out
-        if torch.is_grad_enabled():
+        if torch.is_grad_enabled() and (q.requires_grad or out.requires_grad):
             _no_graph(q, out)
         key = (q.shape, q.stride(), q.dtype, q.get_device(), table.shape, table.stride(), table.dtype, table.get_device(),
                lens.shape, lens.stride(), lens.dtype, lens.get_device(), out.shape, out.stride(), out.dtype, out.get_device())
