@@ -254,7 +254,8 @@ meda_status meda_decode_attention_fp8(const meda_decode_params* params, const vo
  * Every access is bounded on the device: a page number outside [0, n_pages) counts as a page without rows (attention
  * skips its positions, writers write nothing there), a slot outside [0, n_pages * page_size) is skipped, a length is
  * clamped to [0, max_blocks * page_size].  What lies behind a row's last position is never used and never written.
- * Pages that two rows of one call write to, or slots that occur twice in one call, hold either value afterwards.
+ * A page that two rows of one call write to, or a slot that occurs twice in one call, holds elements of either row afterwards;
+ * of 8-bit rows it may hold the codes of one beside the scale of the other, which is neither: give every place one writer.
  * The current device of the calling thread is that of hip_stream; calls that share a workspace must not overlap.
  */
 typedef struct {
@@ -391,7 +392,8 @@ meda_status meda_paged_store(const meda_page_pool* pool, const meda_store_params
  *   table    row r at r * table_stride (0 = max_blocks); lens: that of row r at r * len_stride (0 = 1)
  *   workspace  256-byte aligned, at least meda_paged_workspace_bytes(pool, params); what it holds before does not matter
  * The work is cut evenly over the chip by the lengths, on the device: rows of very different lengths and a captured launch
- * whose lengths grow are served alike.  A row's result depends on the other rows of the call by the rounding of fp32 sums.
+ * whose lengths grow are served alike; a run of empty rows between two long ones can cost 0.1 us a row.  A row's result depends
+ * on the other rows of the call by the rounding of fp32 sums.
  */
 typedef struct {
   int64_t q_stride, out_stride, table_stride, len_stride;

@@ -151,8 +151,10 @@ static hipError_t launch_rotary(RotaryArgs a, hipStream_t s) {
   a.heads_per_part = (int)((heads + parts - 1) / parts);
   const unsigned n_parts = (unsigned)((heads + a.heads_per_part - 1) / a.heads_per_part);
   const dim3 grid((unsigned)groups, n_parts), block(256);
-  // Rows that do not fit the 256 MB of the last-level cache are gone before anybody reads them there (306 MB: 123 us with
-  // ordinary stores, 119 past the caches; 84 MB: 31 and 32).
+  // Rows that fit the 256 MB of the last-level cache stay there for whoever reads them next; others are gone before that, and go
+  // past the caches.  (Bytes written, us with ordinary stores and past the caches, bf16 / fp32: 64 MB 29 and 30 / 27 and 28, 128 MB
+  // 59 and 56 / 57 and 53, 256 MB 111 and 101 / 113 and 106, 320 MB 137 and 125 / 137 and 127, 640 MB 271 and 253 / 271 and 254,
+  // 1600 MB 654 and 602 / 671 and 631.)
   if constexpr (TO == kToRows) {
     if (a.tokens * heads * D * (long long)sizeof(T) >= (256ll << 20)) {
       hipLaunchKernelGGL((rotary_kernel<T, D, TO, true>), grid, block, 0, s, a);
