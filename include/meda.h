@@ -401,7 +401,7 @@ typedef struct {
   int32_t n_q_heads;       /* Hq, Hq % Hkv == 0, Hq / Hkv <= 16                                         */
   int32_t max_blocks;      /* >= 1; max_blocks * page_size <= 2^29, times Hkv and rows <= 2^34          */
   int32_t dtype;
-  float softmax_scale;     /* 0 -> 1/sqrt(head_dim)                                                     */
+  float softmax_scale;     /* 0 -> 1/sqrt(head_dim); times log2(e) finite                               */
 } meda_paged_params;
 size_t meda_paged_workspace_bytes(const meda_page_pool* pool, const meda_paged_params* params);
 meda_status meda_paged_attention(const meda_page_pool* pool, const meda_paged_params* params, const void* q,

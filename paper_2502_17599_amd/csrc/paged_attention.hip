@@ -697,6 +697,8 @@ struct PagedPlan {
   size_t part_bytes, mz_bytes, ws_bytes;
 };
 
+constexpr double kLog2E = 1.4426950408889634074;
+
 static meda_status make_paged_plan(const meda_page_pool* pool, const meda_paged_params* p, PagedPlan* pl) {
   if (!p) return MEDA_ERR_INVALID_ARG;
   meda_status st = check_pool_sizes(pool);
@@ -704,7 +706,8 @@ static meda_status make_paged_plan(const meda_page_pool* pool, const meda_paged_
   if (p->n_rows < 1 || p->n_q_heads < 1 || p->max_blocks < 1) return MEDA_ERR_INVALID_ARG;
   if (p->q_stride < 0 || p->out_stride < 0 || p->table_stride < 0 || p->len_stride < 0) return MEDA_ERR_INVALID_ARG;
   if (p->n_q_heads % pool->n_kv_heads != 0) return MEDA_ERR_INVALID_ARG;
-  if (!(p->softmax_scale >= 0.0f) || !isfinite(p->softmax_scale)) return MEDA_ERR_INVALID_ARG;
+  // (as the kernels use it, times log2(e), it has to be finite too: 0 times infinity is the weight of no maximum)
+  if (!(p->softmax_scale >= 0.0f) || !((double)p->softmax_scale * kLog2E <= (double)__FLT_MAX__)) return MEDA_ERR_INVALID_ARG;
   st = check_types(p->dtype, pool->dtype);
   if (st != MEDA_OK) return st;
   const int G = p->n_q_heads / pool->n_kv_heads;
@@ -800,7 +803,7 @@ meda_status meda_paged_attention(const meda_page_pool* pool, const meda_paged_pa
   a.R = p.n_rows; a.Hq = p.n_q_heads; a.Hkv = pool->n_kv_heads; a.G = a.Hq / a.Hkv; a.max_blocks = p.max_blocks;
   a.cut_by_pair = (int64_t)p.n_rows * pool->n_kv_heads <= pl.groups;
   const double scale = p.softmax_scale > 0.0f ? (double)p.softmax_scale : 1.0 / sqrt((double)pool->head_dim);
-  a.scale_log2 = (float)(scale * 1.4426950408889634074);
+  a.scale_log2 = (float)(scale * kLog2E);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const bool wide = pool->head_dim == 128;
   hipError_t e;
