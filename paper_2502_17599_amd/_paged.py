@@ -55,7 +55,7 @@ class _Kept:
     stream still use it."""
 
     def __init__(self, device: int, tensors):
-        self._device, self._tensors = device, [t for t in tensors if t is not None]
+        self._device, self._tensors = device, tensors
         self._streams = {torch._C._cuda_getCurrentRawStream(device)}
 
     def used_on(self, stream) -> None:
@@ -64,6 +64,15 @@ class _Kept:
             for t in self._tensors:
                 t.record_stream(torch.cuda.current_stream(self._device) if stream is None else stream)
             self._streams.add(raw)
+
+
+def _lend(device: int, stream, *tensors) -> None:
+    """The tensors of a call on a stream that is not the current one: dropped after the call, their memory is not given away
+    before that stream is done with it."""
+    if stream.cuda_stream != torch._C._cuda_getCurrentRawStream(device):
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
 
 
 # A call of a kind that was checked before (the same shapes, strides, types and devices) is not checked again: half of the
@@ -171,6 +180,7 @@ class PagePool:
         if not k_pages.is_cuda:
             raise ValueError("k_pages, v_pages: expected tensors on the GPU")
         self.k_pages, self.v_pages, self.k_scales, self.v_scales = k_pages, v_pages, k_scales, v_scales
+        self.tensors = (k_pages, v_pages) if k_scales is None else (k_pages, v_pages, k_scales, v_scales)
         self.device, self.page_size, self.n_kv_heads, self.head_dim, self.n_pages = k_pages.device, page, heads, d, n
         # the type of the rows that are written to the pages and of the queries that read them
         self.row_dtype = torch.float32 if k_pages.dtype == torch.float32 else torch.bfloat16
@@ -259,6 +269,8 @@ def meda_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Ten
         _written(q_out)
     if new_k is None and k_out is not None:
         _written(k_out)
+    if stream is not None:
+        _lend(dev, stream, q, k, positions, rope.inv_freq, rope.axis, q_out, k_out)
     _call(load_library().meda_rotary, dev, stream, params, pq, pk, positions.data_ptr(), rope.inv_freq.data_ptr(), _p(rope.axis), po, pko)
     return q_out, k_out
 
@@ -323,6 +335,10 @@ def meda_paged_append(pool: PagePool, k: torch.Tensor, v: torch.Tensor, slots: t
                 _want_no_overlap("q_out", q_out, name, t, name == "q")
     if new_q is None and q_out is not None:
         _written(q_out)
+    if stream is not None:
+        _lend(pool.index, stream, k, v, slots, q, q_out, *pool.tensors)
+        if rope is not None:
+            _lend(pool.index, stream, positions, rope.inv_freq, rope.axis)
     turn = (None, None, None) if rope is None else (positions.data_ptr(), rope.inv_freq.data_ptr(), _p(rope.axis))
     _call(load_library().meda_paged_append, pool.index, stream, pool.ref, params, _p(q), k.data_ptr(), v.data_ptr(), *turn, slots.data_ptr(), po)
     return q_out
@@ -388,6 +404,8 @@ def meda_paged_store(pool: PagePool, cache: CompressedCache, table: torch.Tensor
     params = _checked.get(key)
     if params is None:
         params = _remember(key, _plan_store(pool, cache, table, lens))
+    if stream is not None:
+        _lend(pool.index, stream, cache.k_out, cache.v_out, cache.layer_len, cache.layer_off, table, lens, *pool.tensors)
     _call(load_library().meda_paged_store, pool.index, stream, pool.ref, params, cache.k_out.data_ptr(), cache.v_out.data_ptr(),
           cache.layer_len.data_ptr(), cache.layer_off.data_ptr(), lens.data_ptr(), table.data_ptr())
 
@@ -448,6 +466,8 @@ class PagedDecoder:
             _want_no_overlap("out", out, "q", q, False)
         _written(out)
         self._kept.used_on(stream)
+        if stream is not None:
+            _lend(pool.index, stream, q, table, lens, out, *pool.tensors)
         _call(load_library().meda_paged_attention, pool.index, stream, pool.ref, params, pq, table.data_ptr(), lens.data_ptr(), po,
               self.workspace.data_ptr(), self._workspace_bytes)
         return out
@@ -494,6 +514,8 @@ def meda_page_update(lens: torch.Tensor, n_new: torch.Tensor, table: torch.Tenso
     params, dev, max_new, need = plan
     if workspace is None:
         workspace = _empty(need, torch.uint8, table.device, stream)
+    if stream is not None:
+        _lend(dev, stream, lens, n_new, table, free_ring, free_state, lens_out, free_state_out, slots, granted, workspace)
     _call(load_library().meda_page_update, dev, stream, params, lens.data_ptr(), n_new.data_ptr(), table.data_ptr(), free_ring.data_ptr(),
           free_state.data_ptr(), lens_out.data_ptr(), free_state_out.data_ptr(), slots.data_ptr() if max_new else None, _p(granted),
           workspace.data_ptr(), workspace.shape[0])
@@ -573,9 +595,8 @@ class PagedCache:
         self._new = torch.zeros((n_seqs, n_layers), dtype=torch.int32, device=dev)
         self._workspace = torch.empty(meda_page_update_workspace_bytes(rows), dtype=torch.uint8, device=dev)
         self.decoder = PagedDecoder(self.pool, n_seqs, n_q_heads, self.max_blocks, None, softmax_scale)
-        p = self.pool
-        self._kept = _Kept(p.index, (p.k_pages, p.v_pages, p.k_scales, p.v_scales, self.table, self.lens, self.granted, self.slots,
-                                     self.free_ring, self.free_state, self._new, self._workspace))
+        self._kept = _Kept(self.pool.index, self.pool.tensors + (self.table, self.lens, self.granted, self.slots, self.free_ring,
+                                                                 self.free_state, self._new, self._workspace))
 
     def _update(self, slots=None):
         meda_page_update(self.lens, self._new.view(-1), self.table, self.free_ring, self.free_state, self.pool.page_size,

@@ -80,7 +80,7 @@ def _given_away(side, kept):
     ranges = [(t.data_ptr(), t.numel() * t.element_size()) for t in kept]
     kept.clear()
     new = [torch.empty(n, dtype=torch.uint8, device=DEV) for _, n in ranges]
-    assert not side.query()
+    assert side is None or not side.query()
     hit = any(a < t.data_ptr() + t.numel() and t.data_ptr() < a + n for a, n in ranges for t in new)
     torch.cuda.synchronize()
     return hit
@@ -121,3 +121,63 @@ def test_a_dropped_caches_memory_is_kept_until_its_stream_is_done():
         kept = [cache.pool.k_pages, cache.pool.v_pages, cache.table, cache.lens, cache.granted, cache.slots, cache.free_ring, cache.free_state]
         del cache
         assert not _given_away(side, kept)
+
+
+def test_what_a_call_was_lent_is_kept_until_its_stream_is_done():
+    """Every tensor of a call on a given stream is dropped right after it, while the stream is still busy."""
+    import paper_2502_17599_amd as pkg
+    T, H, D, page, n = 300, 4, 64, 16, 40
+
+    def rope():
+        return pkg.RotaryPlan(torch.ones(D // 2, dtype=torch.float64, device=DEV), torch.zeros(D // 2, dtype=torch.uint8, device=DEV), 2)
+
+    def rotary(side):
+        plan = rope()
+        t = [normal(1, T, H, D), normal(2, T, H, D), torch.zeros((2, T), dtype=torch.int32, device=DEV), torch.empty(T, H, D, device=DEV), torch.empty(T, H, D, device=DEV)]
+        return t + [plan.inv_freq, plan.axis], lambda: pkg.meda_rotary(t[0], t[1], t[2], plan, t[3], t[4], stream=side)
+
+    def append(side):
+        plan, pool = rope(), make_pool("fp8", n, H, page, D)
+        t = [normal(i, T, H, D, dtype="bf16") for i in range(4)] + [torch.arange(T, device=DEV), torch.zeros((2, T), dtype=torch.int32, device=DEV)]
+        return t + [plan.inv_freq, plan.axis, *pool.tensors], lambda: pkg.meda_paged_append(pool, t[0], t[1], t[4], t[2], t[5], plan, t[3], stream=side)
+
+    def store(side):
+        pool = make_pool("f32", n, H, page, D)
+        cc, _ = _cache([[300]], H, D, "f32", False, 3)
+        table, lens = make_table([300], page, n)
+        return [cc.k_out, cc.v_out, cc.layer_len, cc.layer_off, table, lens, *pool.tensors], lambda: pkg.meda_paged_store(pool, cc, table, lens, stream=side)
+
+    def attention(side):
+        pool = make_pool("fp8", n, H, page, D)
+        table, lens = make_table([300, 200], page, n)
+        q = normal(4, 2, 2 * H, D, dtype="bf16")
+        out, dec = torch.empty_like(q), pkg.PagedDecoder(pool, 2, 2 * H, table.shape[1])
+        return [q, out, table, lens, dec.workspace, *pool.tensors], lambda: dec(q, table, lens, out, stream=side)
+
+    def update(side):
+        R = 64
+        t = [torch.zeros(R, dtype=torch.int32, device=DEV) for _ in range(4)] + [torch.zeros((R, 9), dtype=torch.int32, device=DEV),
+             torch.arange(900, dtype=torch.int32, device=DEV), torch.tensor([0, 900], device=DEV), torch.zeros(2, dtype=torch.int64, device=DEV),
+             torch.zeros((R, 3), dtype=torch.int64, device=DEV), torch.zeros(pkg.meda_page_update_workspace_bytes(R), dtype=torch.uint8, device=DEV)]
+        return t, lambda: pkg.meda_page_update(t[0], t[1], t[4], t[5], t[6], page, t[2], t[7], t[8], t[3], t[9], side)
+
+    for make in (rotary, append, store, attention, update):
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        kept, call = make(None)                   # on the current stream: what is dropped serves its next tensors
+        call()
+        kept = list(kept)
+        del call
+        assert _given_away(None, kept), make.__name__
+        torch.cuda.empty_cache()
+        side = torch.cuda.Stream()
+        kept, call = make(side)
+        call()                                    # (loads the kernel before the stream is made busy)
+        torch.cuda.synchronize()
+        kept, call = make(side)
+        torch.cuda.synchronize()
+        _late(side)
+        call()
+        kept = list(kept)
+        del call
+        assert not _given_away(side, kept), make.__name__
