@@ -426,6 +426,8 @@ def _plan_store(pool, cache, table, lens):
     R, blocks, ts, ls = _want_table(table, lens, dev)
     if R != N * L:
         raise ValueError(f"table: expected {N * L} rows, one per sequence and layer")
+    if R * -(-blocks * pool.page_size // 16) * pool.n_kv_heads >= 1 << 31:
+        raise ValueError(f"table: {R} rows of {blocks * pool.page_size} positions in {pool.n_kv_heads} heads are more than 2^34 together")
     return ctypes.byref(MedaStoreParams(rows, ts, ls, N, L, blocks, _DTYPES[dt]))
 
 
@@ -611,7 +613,11 @@ class PagedCache:
             raise ValueError(f"expected {self.n_layers} layers and sequences below {self.n_seqs}")
         rows = slice(first * layers, (first + n) * layers)
         table, lens = self.table[rows], self.lens[rows]
-        _plan_store(self.pool, cache, table, lens)      # (a cache that does not fit is refused before anything changes)
+        _plan_store(self.pool, cache, table, lens)      # (a cache that the store would not take is refused before anything changes)
+        if cache.k_out.data_ptr() % 16 or cache.v_out.data_ptr() % 16:
+            raise ValueError("k_out, v_out: expected memory aligned to 16 bytes")
+        if torch.is_grad_enabled():
+            _no_graph(cache.k_out, cache.v_out)
         self.release(range(first, first + n))
         self._new.zero_()
         self._new[first:first + n].copy_(layer_len)
